@@ -299,6 +299,116 @@ int bpd_profile_samples(bpd_ctx* ctx, float* ms_out, int64_t capacity, double* t
 int bpd_measure_hbm_read(void* buf_dev, size_t bytes, void* hip_stream, int iters, double* gbps);
 int bpd_measure_mfma_bf16(void* scratch_dev, void* hip_stream, int iters, double* tflops);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators on caches of keys and values that the caller owns: what a serving loop of its own needs
+ * around them.  No context: they run on the current device and on hip_stream (NULL: the default stream),
+ * only enqueue, allocate nothing, and can be captured into a HIP graph.  All pointers are [device] unless
+ * said otherwise; what is wrong with the arguments (on the host: null pointers, sizes, alignment) is
+ * returned before anything is enqueued, with a message in bpd_op_error().  Values in device memory are not
+ * trusted: lengths, counts and parents of any value touch nothing outside the arrays.  Results do not
+ * depend on the order in which workgroups run: the same call gives the same bits.
+ *
+ * Two calls may overlap if neither writes what the other uses (a workspace belongs to one call at a time;
+ * graphs that are replayed one behind the other may share it). */
+
+/* Keys and values of n_layers layers, a layer behind the other.
+ *   BPD_BF16, head_dim 64 or 128: operand order, [layer][max_batch][n_kv_heads][capacity / 32] groups of
+ *     32 keys, each 32 * head_dim elements (capacity a multiple of 32):
+ *       K  [t < 2][s < head_dim / 32][q < 4][a < 4][r < 4][e < 8]  = key 8 a + 4 t + r, dimension 32 s + 8 q + e
+ *       V  [s < head_dim / 16][q < 4][c < 16][e < 8]               = key 8 q + e,       dimension 16 s + c
+ *   BPD_BF16 of head_dim 16, and BPD_F32 of head_dim 16, 64 or 128: [layer][max_batch][capacity][n_kv_heads][head_dim].
+ * Row r of a sequence holds the key and value at position r.  k, v: 16-byte aligned, bpd_cache_bytes() each.
+ * What rows hold that nothing has been stored in does not matter. */
+typedef struct {
+  void* k; void* v;
+  int32_t dtype, n_layers, max_batch, n_kv_heads, head_dim, capacity;   /* max_batch <= 65535, n_kv_heads <= 1024, capacity <= 2^24 */
+} bpd_cache;
+
+/* Rows of some heads: element c of head h of row t of sequence b (of layer l) at data + l * layer + b * seq + t * row +
+ * h * head + c.  Strides in elements, of any value (several rows may read the same ones); rows that start
+ * at multiples of 16 bytes move fastest. */
+typedef struct {
+  const void* data;        /* written to where it is a result                                 */
+  int32_t dtype;           /* BPD_F32 or BPD_BF16                                             */
+  int64_t layer, seq, row, head;
+} bpd_rows;
+
+#define BPD_TREE_MAX   64     /* nodes of a tree of drafts                                       */
+#define BPD_BLOCKS_MAX 4096   /* blocks of a cache that bpd_sparse_attention chooses from        */
+
+/* Message of the last cache operator of this thread that returned an error. */
+const char* bpd_op_error(void);
+
+/* Bytes of k (and of v); of the summaries of all blocks of one layer; of the workspace of an attention of T
+ * nodes in each of B sequences with n_heads query heads (block 0: bpd_tree_attention, otherwise
+ * bpd_sparse_attention with blocks of so many rows), on the current device.  0: sizes that the operators refuse,
+ * or nothing needed (pointers are not looked at). */
+size_t bpd_cache_bytes(const bpd_cache* cache);
+size_t bpd_summaries_bytes(const bpd_cache* cache, int block);
+size_t bpd_attention_workspace_bytes(const bpd_cache* cache, int B, int T, int n_heads, int block);
+
+/* Store rows 0 .. count[b] - 1 of k and v (head h: key head h) as rows start[b] .. of sequence b, in all
+ * layers of the cache, rounded to its dtype (nearest even).  count null: T each; start[b] < 0: none; rows
+ * at and past the capacity are left out.  Rows not named keep their bits.
+ * Errors: BPD_E_ARG, BPD_E_CAPACITY (T over the capacity, B * n_layers over 65535), BPD_E_HIP. */
+int bpd_cache_store(const bpd_cache* cache, const bpd_rows* k, const bpd_rows* v, const int32_t* start,
+                    const int32_t* count, int B, int T, void* hip_stream);
+
+/* Attention of a tree of drafted tokens (Section 3's block is a chain) over the first layer of a cache:
+ * sequence b has length[b] committed rows, and behind them, stored already, the rows of its T nodes (node i
+ * at row length[b] + i).
+ *   parent [B, T] or NULL (a chain, parent i - 1): -1: node i follows the prefix; 0 .. i - 1: that node.  Any other value: node i is
+ *       absent (trees of fewer nodes, padded).  Absent as well: nodes below an absent one, rows past the
+ *       capacity, all nodes of a sequence with length[b] < 0.
+ *   q, out  rows of n_heads heads (a multiple of the cache's: heads in a row share a key head)
+ *   out[b][i][h] = sum_j p_j V_j,  p = softmax of scale * q . K_j over the prefix and node i's ancestors and itself;
+ *       0 for absent nodes.  Sums, maxima and weights in fp32; what no node sees does not matter, NaN or not.
+ *       (A value that is not finite, in a row that only other nodes of the tree see, may reach all results of its head.)
+ * Chains of one node are plain decoding.  T <= BPD_TREE_MAX; n_heads / n_kv_heads <= 64; B or T of 0 does nothing.
+ * Errors: BPD_E_ARG, BPD_E_CAPACITY (workspace), BPD_E_HIP. */
+int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows* out, const int32_t* length,
+                       const int32_t* parent, int B, int T, int n_heads, float scale,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Which blocks of the prefix bpd_sparse_attention sees.  The prefix is cut in blocks of `block` rows, of which
+ * n = length / block are complete.  Seen: the first `first`, the last `recent` of them, and of the others
+ * the `top` with the largest bound of the scores in them, for each node and key head:
+ *     sum over the group's heads of  sum_c max(q_c min_c, q_c max_c),   min, max over the block's keys,
+ * in 64 bits, ties to the lower block, a bound that is NaN last.  Rows behind the last complete block are always seen. */
+typedef struct {
+  int32_t block;           /* 32, 64 or 128 rows                                              */
+  int32_t first, recent, top;
+  void* summaries;         /* smallest and largest key of every block, the cache's dtype, kept by the caller from call to
+                              call (one buffer per layer), 16-byte aligned, bpd_summaries_bytes():
+                              [max_batch][n_kv_heads][tiles of 64 blocks][2][head_dim / 8][64][8]   */
+  const int32_t* added;    /* [B] rows committed since the call before: the complete blocks that rows
+                              length - added .. length - 1 lie in are summarised anew.  NULL: all of them
+                              (the first call, and after anything else)                       */
+  uint32_t* chosen;        /* NULL, or [B][n_kv_heads][T][ceil(floor(capacity / block) / 32)]: bit j of word w: block 32 w + j is seen */
+} bpd_blocks;
+
+/* As bpd_tree_attention, with the prefix seen by the chosen blocks only.
+ * Errors: as there, and BPD_E_CAPACITY (capacity / block over BPD_BLOCKS_MAX). */
+int bpd_sparse_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows* out, const int32_t* length,
+                         const int32_t* parent, int B, int T, int n_heads, float scale, const bpd_blocks* blocks,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Verification of a tree (Section 3's acceptance along its branches): from the prefix on, the first child of the
+ * last accepted node whose token is p_1's choice there, and so on: the longest path that greedy decoding takes.
+ *   parent, token [B, T]   as above; the nodes' tokens
+ *   expect [B]             p_1's choice behind the prefix;  best [B, T]  p_1's choice behind each node
+ *   length [B]             committed rows;  room [B] or NULL: at most so many are accepted
+ *   eos_id                 the path ends behind this token (< 0: none does)
+ *   path [B, T]            accepted nodes, -1 behind them;  accepted [B]  their number
+ *   next [B]               p_1's choice behind the last accepted node (none: expect)
+ *   new_length [B]         length + accepted (a negative length: nothing is accepted, and it stays)
+ *   cache                  NULL, or the cache whose rows length + path[m] move to length + m, in all layers; nodes whose rows
+ *                          are past its capacity are then absent
+ * The four results must not overlap what is read.  Errors: BPD_E_ARG, BPD_E_CAPACITY (n_layers over 65535), BPD_E_HIP. */
+int bpd_tree_accept(const int32_t* parent, const int32_t* token, const int32_t* expect, const int32_t* best,
+                    const int32_t* length, const int32_t* room, int eos_id, int B, int T, int32_t* path,
+                    int32_t* accepted, int32_t* next, int32_t* new_length, const bpd_cache* cache, void* hip_stream);
+
 const char* bpd_last_error(const bpd_ctx* ctx);
 
 #ifdef __cplusplus

@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbpd.so")
 
 BPD_F32, BPD_BF16 = 0, 1
+TREE_MAX, BLOCKS_MAX = 64, 4096          # nodes of a tree, blocks that are chosen from
 PHASE_NONE, PHASE_LAYERS, PHASE_HEAD_HIDDEN, PHASE_HEAD_OUT, PHASE_VOCAB, PHASE_ACCEPT, PHASE_STEP, PHASE_EMPTY = range(8)
 ERRORS = {-1: "BPD_E_ARG", -2: "BPD_E_STATE", -3: "BPD_E_CAPACITY", -4: "BPD_E_WEIGHTS", -5: "BPD_E_HIP"}
 
@@ -41,10 +42,25 @@ class bpd_stats(C.Structure):
                 ("accepted_total", C.c_int64), ("hist", C.c_int64 * 17), ("finished", C.c_int32)]
 
 
+class bpd_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "dtype", "n_layers", "max_batch", "n_kv_heads", "head_dim", "capacity")]
+
+
+class bpd_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32)] + [(n, C.c_int64) for n in ("layer", "seq", "row", "head")]
+
+
+class bpd_blocks(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("block", "first", "recent", "top")] + [(n, C.c_void_p) for n in ("summaries", "added", "chosen")]
+
+
 EXPORTS = ["bpd_workspace_bytes", "bpd_create", "bpd_destroy", "bpd_load_weights", "bpd_encode", "bpd_step", "bpd_step_static",
            "bpd_set_acceptance", "bpd_set_top_n", "bpd_set_two_phase", "bpd_set_local_attention", "bpd_decode", "bpd_get_state", "bpd_get_output", "bpd_get_stats",
            "bpd_set_proposals", "bpd_debug_step_logits", "bpd_profile_enable", "bpd_profile_read",
-           "bpd_profile_samples", "bpd_measure_hbm_read", "bpd_measure_mfma_bf16", "bpd_last_error"]
+           "bpd_profile_samples", "bpd_measure_hbm_read", "bpd_measure_mfma_bf16", "bpd_last_error",
+           "bpd_op_error", "bpd_cache_bytes", "bpd_summaries_bytes", "bpd_attention_workspace_bytes", "bpd_cache_store", "bpd_tree_attention",
+           "bpd_sparse_attention", "bpd_tree_accept"]
 
 _lib = None
 
@@ -82,6 +98,15 @@ def lib() -> C.CDLL:
         L.bpd_profile_samples.argtypes = [vp, vp, C.c_int64, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.bpd_measure_hbm_read.argtypes = [vp, C.c_size_t, vp, C.c_int, C.POINTER(C.c_double)]
         L.bpd_measure_mfma_bf16.argtypes = [vp, vp, C.c_int, C.POINTER(C.c_double)]
+        cp, rp, sz = C.POINTER(bpd_cache), C.POINTER(bpd_rows), C.c_size_t
+        L.bpd_op_error.restype = C.c_char_p
+        L.bpd_op_error.argtypes = []
+        for name, args in (("bpd_cache_bytes", [cp]), ("bpd_summaries_bytes", [cp, C.c_int]), ("bpd_attention_workspace_bytes", [cp] + [C.c_int] * 4)):
+            getattr(L, name).restype, getattr(L, name).argtypes = sz, args
+        L.bpd_cache_store.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, vp]
+        L.bpd_tree_attention.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, sz, vp]
+        L.bpd_sparse_attention.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, C.POINTER(bpd_blocks), vp, sz, vp]
+        L.bpd_tree_accept.argtypes = [vp] * 6 + [C.c_int] * 3 + [vp] * 4 + [cp, vp]
         L.bpd_last_error.restype = C.c_char_p
         L.bpd_last_error.argtypes = [vp]
         _lib = L
@@ -123,6 +148,139 @@ def _i32(a):
     import torch
     assert a.dtype == torch.int32
     return a.contiguous()
+
+
+# -- caches that the caller owns
+def new_cache(max_batch: int, n_kv_heads: int, head_dim: int, capacity: int, dtype=None, device="cuda", n_layers: Optional[int] = None):
+    """(k, v): empty cache tensors of the shapes that the cache operators take, [n_layers,] B, .. (bpd_cache in include/bpd.h).
+    bf16 heads of 64 and 128 dimensions: [B, heads, capacity / 32, 32, head_dim] in operand order, the capacity rounded up to a multiple of 32;
+    others: [B, capacity, heads, head_dim]."""
+    import torch
+    dtype = dtype or torch.bfloat16
+    if dtype == torch.bfloat16 and head_dim in (64, 128):
+        shape = (max_batch, n_kv_heads, (capacity + 31) // 32, 32, head_dim)
+    else:
+        shape = (max_batch, capacity, n_kv_heads, head_dim)
+    shape = shape if n_layers is None else (n_layers,) + shape
+    return torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
+
+
+def new_summaries(cache, block: int):
+    """Summaries of one layer's blocks for bpd_sparse_attention, zeros."""
+    import torch
+    c, k, _ = _cache(cache, 0)
+    tiles = (c.capacity // block + 63) // 64
+    return torch.zeros((c.max_batch, c.n_kv_heads, tiles, 2, c.head_dim // 8, 64, 8), dtype=k.dtype, device=k.device)
+
+
+def _op_check(rc: int):
+    if rc != 0:
+        raise BpdError(rc, lib().bpd_op_error().decode())
+
+
+def _bad(what: str):
+    return BpdError(-1, what)
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BPD_BF16
+    if t.dtype == torch.float32:
+        return BPD_F32
+    raise _bad(f"tensors are bfloat16 or float32, not {t.dtype}")
+
+
+def _cache(cache, layer: Optional[int] = None):
+    """bpd_cache of the tensors (k, v); layer: of that one alone.  Returns (struct, k, whether the tensors have a dimension of layers)."""
+    k, v = cache
+    dtype, d = _dtype_of(k), k.shape[-1]
+    grouped = dtype == BPD_BF16 and d in (64, 128)
+    layers = k.dim() - (5 if grouped else 4)
+    if layers not in (0, 1) or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or not k.is_contiguous() or not v.is_contiguous():
+        raise _bad("cache: k and v are contiguous tensors of one shape, type and device, as binding.new_cache makes them")
+    n = k.shape[0] if layers else 1
+    kp, vp = k.data_ptr(), v.data_ptr()
+    if grouped:
+        b, h, groups, rows, _ = k.shape[layers:]
+        if rows != 32:
+            raise _bad("cache: groups of 32 keys")
+        cap = 32 * groups
+    else:
+        b, cap, h, _ = k.shape[layers:]
+    if layer is not None:
+        if not 0 <= layer < n:
+            raise _bad("cache: no such layer")
+        at = layer * (b * h * cap * d) * k.element_size()
+        kp, vp, n = kp + at, vp + at, 1
+    return bpd_cache(kp, vp, dtype, n, b, h, d, cap), k, layers
+
+
+def _same(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise _bad(f"{name} is on {t.device}, the cache on {device}")
+
+
+def _ints(shape, **tensors):
+    """Device int32 arrays of the given shape, contiguous."""
+    import torch
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise _bad(f"{name}: contiguous int32 {list(shape)}")
+
+
+def _rows(t, layers: int = 0):
+    """bpd_rows of a tensor [layers,] B, T, heads, D whose last dimension is contiguous."""
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise _bad("the last dimension of rows is contiguous")
+    s = t.stride()
+    return bpd_rows(t.data_ptr(), _dtype_of(t), s[0] if layers else 0, s[layers], s[layers + 1], s[layers + 2])
+
+
+class _on:
+    """The device of a tensor as the current one, and torch's current stream there."""
+
+    def __init__(self, device):
+        import torch
+        if device.type != "cuda":
+            raise _bad("tensors are on a GPU")
+        self.guard = torch.cuda.device(device) if device.index not in (None, torch.cuda.current_device()) else None
+        self.stream = torch.cuda.current_stream(device).cuda_stream
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *a):
+        if self.guard:
+            self.guard.__exit__(*a)
+
+
+def _attention(cache, layer, q, length, parent, scale, out, workspace, block):
+    """What both attentions do with their arguments: (cache, q, out as structs, B, T, heads, scale, workspace, out)."""
+    import torch
+    c, k, _ = _cache(cache, layer)
+    if q.dim() != 4 or q.shape[-1] != c.head_dim:
+        raise _bad("q: [B, T, heads, head_dim]")
+    b, t, h, d = q.shape
+    if out is None:
+        out = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise _bad("out: the shape of q")
+    _same(k.device, q=q, out=out, length=length, parent=parent, workspace=workspace)
+    _ints((b,), length=length)
+    _ints((b, t), parent=parent)
+    return c, _rows(q), _rows(out), b, t, h, (d ** -0.5 if scale is None else float(scale)), out
+
+
+def _workspace(c, b, t, h, block, workspace, device):
+    import torch
+    need = lib().bpd_attention_workspace_bytes(C.byref(c), b, t, h, block)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    return workspace, (workspace.data_ptr() if workspace is not None else None), (workspace.numel() * workspace.element_size() if workspace is not None else 0)
 
 
 class Context:
@@ -296,3 +454,84 @@ class Context:
         if rc:
             raise BpdError(rc, "bpd_measure_mfma_bf16")
         return tf.value
+
+    # -- operators on caches of the caller's (no context; torch's current stream of the tensors' device)
+    @staticmethod
+    def bpd_op_error() -> str:
+        return lib().bpd_op_error().decode()
+
+    @staticmethod
+    def bpd_cache_bytes(cache) -> int:
+        return lib().bpd_cache_bytes(C.byref(_cache(cache)[0]))
+
+    @staticmethod
+    def bpd_summaries_bytes(cache, block: int) -> int:
+        return lib().bpd_summaries_bytes(C.byref(_cache(cache, 0)[0]), block)
+
+    @staticmethod
+    def bpd_attention_workspace_bytes(cache, B: int, T: int, n_heads: int, block: int = 0) -> int:
+        c, k, _ = _cache(cache, 0)
+        with _on(k.device):
+            return lib().bpd_attention_workspace_bytes(C.byref(c), B, T, n_heads, block)
+
+    @staticmethod
+    def bpd_cache_store(cache, k, v, start, count=None):
+        """Rows k, v [B, T, kv heads, head_dim] ([n_layers, B, ..] for a cache with layers) to rows start[b] .. of the cache; count[b] of them (None: T)."""
+        c, kc, layers = _cache(cache)
+        if k.dim() != 4 + layers or k.shape != v.shape or k.shape[-1] != c.head_dim or k.shape[-2] != c.n_kv_heads or (layers and k.shape[0] != c.n_layers):
+            raise _bad("k, v: [B, T, kv heads, head_dim], behind the layers if the cache has any")
+        b, t = k.shape[layers:layers + 2]
+        _same(kc.device, k=k, v=v, start=start, count=count)
+        _ints((b,), start=start, count=count)
+        with _on(kc.device) as stream:
+            _op_check(lib().bpd_cache_store(C.byref(c), C.byref(_rows(k, layers)), C.byref(_rows(v, layers)), start.data_ptr(), None if count is None else count.data_ptr(), b, t, stream))
+
+    @staticmethod
+    def bpd_tree_attention(cache, q, length, parent=None, layer: int = 0, scale: Optional[float] = None, out=None, workspace=None):
+        """q [B, T, heads, head_dim], length [B], parent [B, T] or None (a chain).  Returns out (of q's dtype, unless given; scale None: head_dim ** -0.5)."""
+        c, qr, outr, b, t, h, scale, out = _attention(cache, layer, q, length, parent, scale, out, workspace, 0)
+        with _on(q.device) as stream:
+            keep, ws, n = _workspace(c, b, t, h, 0, workspace, q.device)
+            _op_check(lib().bpd_tree_attention(C.byref(c), C.byref(qr), C.byref(outr), length.data_ptr(), None if parent is None else parent.data_ptr(), b, t, h, scale, ws, n, stream))
+        return out
+
+    @staticmethod
+    def bpd_sparse_attention(cache, q, length, summaries, block: int, first: int, recent: int, top: int, parent=None, added=None, layer: int = 0,
+                             scale: Optional[float] = None, out=None, chosen=None, workspace=None):
+        """As bpd_tree_attention, over chosen blocks; summaries: binding.new_summaries(), one per layer.  Returns (out, chosen [B, kv heads, T, words] int32)."""
+        import torch
+        c, qr, outr, b, t, h, scale, out = _attention(cache, layer, q, length, parent, scale, out, workspace, block)
+        _same(q.device, summaries=summaries, added=added, chosen=chosen)
+        _ints((b,), added=added)
+        if lib().bpd_summaries_bytes(C.byref(c), block) != summaries.numel() * summaries.element_size() or not summaries.is_contiguous():
+            raise _bad("block: 32, 64 or 128 rows; summaries: as binding.new_summaries makes them")
+        words = (c.capacity // block + 31) // 32
+        if chosen is None:
+            chosen = torch.empty((b, c.n_kv_heads, t, words), dtype=torch.int32, device=q.device)
+        _ints((b, c.n_kv_heads, t, words), chosen=chosen)
+        blocks = bpd_blocks(block, first, recent, top, summaries.data_ptr(), None if added is None else added.data_ptr(), chosen.data_ptr())
+        with _on(q.device) as stream:
+            keep, ws, n = _workspace(c, b, t, h, block, workspace, q.device)
+            _op_check(lib().bpd_sparse_attention(C.byref(c), C.byref(qr), C.byref(outr), length.data_ptr(), None if parent is None else parent.data_ptr(), b, t, h, scale,
+                                                 C.byref(blocks), ws, n, stream))
+        return out, chosen
+
+    @staticmethod
+    def bpd_tree_accept(parent, token, expect, best, length, cache=None, room=None, eos_id: int = -1, out=None):
+        """parent, token, best [B, T], expect, length, room [B].  Returns (path [B, T], accepted [B], next [B], new_length [B]), or writes them to `out`."""
+        import torch
+        if parent.dim() != 2:
+            raise _bad("parent: [B, T]")
+        b, t = parent.shape
+        if out is None:
+            out = (torch.empty_like(parent), torch.empty_like(length), torch.empty_like(length), torch.empty_like(length))
+        path, accepted, following, new_length = out
+        _same(parent.device, token=token, expect=expect, best=best, length=length, room=room, path=path, accepted=accepted, next=following, new_length=new_length,
+              cache=None if cache is None else cache[0])
+        _ints((b, t), parent=parent, token=token, best=best, path=path)
+        _ints((b,), expect=expect, length=length, room=room, accepted=accepted, next=following, new_length=new_length)
+        c = None if cache is None else C.byref(_cache(cache)[0])
+        with _on(parent.device) as stream:
+            _op_check(lib().bpd_tree_accept(parent.data_ptr(), token.data_ptr(), expect.data_ptr(), best.data_ptr(), length.data_ptr(), None if room is None else room.data_ptr(), eos_id, b, t,
+                                            path.data_ptr(), accepted.data_ptr(), following.data_ptr(), new_length.data_ptr(), c, stream))
+        return out

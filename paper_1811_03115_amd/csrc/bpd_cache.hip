@@ -1,0 +1,243 @@
+// Host side of the cache operators of include/bpd.h: checks of their arguments, sizes, launches.  They take no context: what they need is in
+// their arguments, and they run on the current device and the stream that they are given.
+#include "../../include/bpd.h"
+#include "bpd_cache_ops.h"
+#include "bpd_cache_logic.h"
+
+#include <atomic>
+#include <cmath>
+#include <string>
+
+namespace {
+
+thread_local std::string op_error;
+
+int refuse(int code, const char* what) {
+  try { op_error = what; } catch (...) {}
+  return code;
+}
+int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return BPD_OK;
+  try { op_error = std::string(what) + ": " + hipGetErrorString(e); } catch (...) {}
+  return BPD_E_HIP;
+}
+// Compute units of the current device
+int compute_units() {
+  static std::atomic<int> known[64];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 256;
+  if (dev >= 0 && dev < 64 && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) return 256;
+  if (dev >= 0 && dev < 64) known[dev].store(cus, std::memory_order_relaxed);
+  return cus;
+}
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// Can four elements (of 2 or 4 bytes) of rows be moved at once, eight of bf16?
+bool rows_aligned(const bpd_rows& r) {
+  const int64_t m = r.dtype == BPD_F32 ? 3 : 7;
+  return aligned16(r.data) && ((r.layer | r.seq | r.row | r.head) & m) == 0;
+}
+const char* rows_wrong(const bpd_rows* r) {
+  if (!r || !r->data) return "rows: null";
+  if (r->dtype != BPD_F32 && r->dtype != BPD_BF16) return "rows: dtype is BPD_F32 or BPD_BF16";
+  if ((uintptr_t)r->data & (r->dtype == BPD_F32 ? 3 : 1)) return "rows: not aligned to an element";
+  return nullptr;
+}
+RowsP rows_of(const bpd_rows& r) { return RowsP{r.data, r.dtype == BPD_F32, rows_aligned(r) ? 1 : 0, (long)r.layer, (long)r.seq, (long)r.row, (long)r.head}; }
+
+template <int D, int MT, bool SPARSE>
+void attend_groups(const TreeP& p, dim3 grid, hipStream_t s) {
+  if (p.q_f32) hipLaunchKernelGGL((tree_attention_kernel<D, MT, true, SPARSE>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tree_attention_kernel<D, MT, false, SPARSE>), grid, dim3(256), 0, s, p);
+}
+template <int D, bool SPARSE>
+void attend_tiles(const TreeP& p, int mt, dim3 grid, hipStream_t s) {
+  if (mt == 1) attend_groups<D, 1, SPARSE>(p, grid, s);
+  else if (mt == 2) attend_groups<D, 2, SPARSE>(p, grid, s);
+  else if constexpr (D == 64) attend_groups<D, 4, SPARSE>(p, grid, s);
+}
+template <bool SPARSE>
+void attend(const bpd_cache& c, const TreeP& p, const TreePlan& plan, hipStream_t s) {
+  const dim3 grid(p.kv * p.nsplit, plan.blocks, p.B);
+  const int D = c.head_dim;
+  if (cache_grouped(c)) {
+    if (D == 64) attend_tiles<64, SPARSE>(p, plan.mt, grid, s); else attend_tiles<128, SPARSE>(p, plan.mt, grid, s);
+  } else if (c.dtype == BPD_BF16) {
+    hipLaunchKernelGGL((tree_rows_kernel<bf16_t, 16, SPARSE>), grid, dim3(256), 0, s, p);
+  } else if (D == 16) {
+    hipLaunchKernelGGL((tree_rows_kernel<float, 16, SPARSE>), grid, dim3(256), 0, s, p);
+  } else if (D == 64) {
+    hipLaunchKernelGGL((tree_rows_kernel<float, 64, SPARSE>), grid, dim3(256), 0, s, p);
+  } else {
+    hipLaunchKernelGGL((tree_rows_kernel<float, 128, SPARSE>), grid, dim3(256), 0, s, p);
+  }
+  if (p.nsplit > 1) {
+    const long rows = (long)p.B * p.kv * p.T * p.G;
+    const int per = 256 / (D / 4), n = (int)((rows + per - 1) / per);
+    if (D == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
+    else if (D == 64) hipLaunchKernelGGL(tree_join_kernel<64>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
+    else hipLaunchKernelGGL(tree_join_kernel<128>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
+  }
+}
+
+// What bpd_tree_attention and bpd_sparse_attention check alike; null: nothing is wrong
+const char* attention_wrong(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, int B, int T, int heads, float scale) {
+  if (const char* w = cache_wrong(c)) return w;
+  if (B < 0 || B > c->max_batch) return "attention: B outside 0..max_batch";
+  if (T < 0 || T > BPD_TREE_MAX) return "attention: T outside 0..BPD_TREE_MAX";
+  if (heads < 1 || heads % c->n_kv_heads || heads / c->n_kv_heads > 64) return "attention: heads are 1 to 64 times the cache's";
+  if (!(scale == scale) || std::isinf(scale)) return "attention: scale is not finite";
+  if (B == 0 || T == 0) return nullptr;          // (nothing is read)
+  if (const char* w = rows_wrong(q)) return w;
+  if (const char* w = rows_wrong(out)) return w;
+  return length ? nullptr : "attention: null length";
+}
+TreeP attention_args(const bpd_cache& c, const bpd_rows& q, const bpd_rows& out, const int32_t* length, const int32_t* parent, int B, int T, int heads, float scale) {
+  TreeP p{};
+  p.q = q.data; p.q_seq = (long)q.seq; p.q_row = (long)q.row; p.q_head = (long)q.head;
+  p.out = const_cast<void*>(out.data); p.o_seq = (long)out.seq; p.o_row = (long)out.row; p.o_head = (long)out.head;
+  p.K = c.k; p.V = c.v;
+  p.B = B; p.T = T; p.H = heads; p.kv = c.n_kv_heads; p.G = heads / c.n_kv_heads; p.cap = c.capacity;
+  p.length = length; p.parent = parent;
+  p.scale = scale * 1.44269504088896340736f;
+  p.q_f32 = q.dtype == BPD_F32; p.o_f32 = out.dtype == BPD_F32;
+  p.vec = rows_aligned(q) && rows_aligned(out);
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* bpd_op_error(void) { return op_error.c_str(); }
+
+size_t bpd_cache_bytes(const bpd_cache* c) {
+  if (cache_sizes_wrong(c)) return 0;
+  return cache_layer_elements(*c) * c->n_layers * cache_element(*c);
+}
+
+size_t bpd_summaries_bytes(const bpd_cache* c, int block) {
+  if (cache_sizes_wrong(c) || block_wrong(*c, block)) return 0;
+  return summaries_elements(*c, block) * cache_element(*c);
+}
+
+size_t bpd_attention_workspace_bytes(const bpd_cache* c, int B, int T, int heads, int block) {
+  if (cache_sizes_wrong(c) || B < 1 || T < 1 || T > BPD_TREE_MAX || heads < 1 || heads % c->n_kv_heads) return 0;
+  if (block && block_wrong(*c, block)) return 0;
+  return plan_attention(*c, B, T, heads, block, compute_units()).bytes;
+}
+
+int bpd_cache_store(const bpd_cache* c, const bpd_rows* k, const bpd_rows* v, const int32_t* start, const int32_t* count, int B, int T, void* hip_stream) {
+  if (const char* w = cache_wrong(c)) return refuse(BPD_E_ARG, w);
+  if (B < 0 || B > c->max_batch || T < 0) return refuse(BPD_E_ARG, "bpd_cache_store: B outside 0..max_batch, or T < 0");
+  if (T > c->capacity) return refuse(BPD_E_CAPACITY, "bpd_cache_store: more rows than the cache has");
+  if ((int64_t)B * c->n_layers > 65535) return refuse(BPD_E_CAPACITY, "bpd_cache_store: more than 65535 sequences times layers");
+  if (B == 0 || T == 0) return BPD_OK;
+  if (const char* w = rows_wrong(k)) return refuse(BPD_E_ARG, w);
+  if (const char* w = rows_wrong(v)) return refuse(BPD_E_ARG, w);
+  if (!start) return refuse(BPD_E_ARG, "bpd_cache_store: null start");
+  StoreP p{rows_of(*k), rows_of(*v), c->k, c->v, (long)cache_layer_elements(*c), B, T, c->n_kv_heads, c->capacity, start, count};
+  const hipStream_t s = (hipStream_t)hip_stream;
+  if (cache_grouped(*c)) {
+    const dim3 grid((T + 30) / 32 + 1, c->n_kv_heads, B * c->n_layers);
+    if (c->head_dim == 64) hipLaunchKernelGGL(store_groups_kernel<64>, grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(store_groups_kernel<128>, grid, dim3(256), 0, s, p);
+  } else {
+    const dim3 grid(T, 1, B * c->n_layers);
+    if (c->dtype == BPD_F32) hipLaunchKernelGGL(store_rows_kernel<float>, grid, dim3(256), 0, s, p, c->head_dim);
+    else hipLaunchKernelGGL(store_rows_kernel<bf16_t>, grid, dim3(256), 0, s, p, c->head_dim);
+  }
+  return launched("bpd_cache_store");
+}
+
+int bpd_tree_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, const int32_t* parent, int B, int T, int heads,
+                       float scale, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const char* w = attention_wrong(c, q, out, length, B, T, heads, scale)) return refuse(BPD_E_ARG, w);
+  if (B == 0 || T == 0) return BPD_OK;
+  const TreePlan plan = plan_attention(*c, B, T, heads, 0, compute_units());
+  if (plan.bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < plan.bytes)) return refuse(BPD_E_CAPACITY, "bpd_tree_attention: workspace too small or not aligned to 16 bytes");
+  TreeP p = attention_args(*c, *q, *out, length, parent, B, T, heads, scale);
+  p.nsplit = plan.nsplit; p.part = (float*)workspace;
+  attend<false>(*c, p, plan, (hipStream_t)hip_stream);
+  return launched("bpd_tree_attention");
+}
+
+int bpd_sparse_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, const int32_t* parent, int B, int T, int heads,
+                         float scale, const bpd_blocks* blocks, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const char* w = attention_wrong(c, q, out, length, B, T, heads, scale)) return refuse(BPD_E_ARG, w);
+  if (!blocks) return refuse(BPD_E_ARG, "bpd_sparse_attention: null blocks");
+  if (const char* w = block_wrong(*c, blocks->block)) return refuse(BPD_E_ARG, w);
+  if (blocks->first < 0 || blocks->recent < 0 || blocks->top < 0) return refuse(BPD_E_ARG, "bpd_sparse_attention: first, recent and top are not negative");
+  const int nb = c->capacity / blocks->block;
+  if (nb > BPD_BLOCKS_MAX) return refuse(BPD_E_CAPACITY, "bpd_sparse_attention: more than BPD_BLOCKS_MAX blocks");
+  if (nb > 0 && (!blocks->summaries || !aligned16(blocks->summaries))) return refuse(BPD_E_ARG, "bpd_sparse_attention: summaries null or not aligned to 16 bytes");
+  if (B == 0 || T == 0) return BPD_OK;
+  const TreePlan plan = plan_attention(*c, B, T, heads, blocks->block, compute_units());
+  if (plan.bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < plan.bytes)) return refuse(BPD_E_CAPACITY, "bpd_sparse_attention: workspace too small or not aligned to 16 bytes");
+  const hipStream_t s = (hipStream_t)hip_stream;
+  TreeP p = attention_args(*c, *q, *out, length, parent, B, T, heads, scale);
+  p.nsplit = plan.nsplit; p.part = (float*)workspace;
+  if (nb == 0) {                                 // nothing to choose from
+    attend<false>(*c, p, plan, s);
+    return launched("bpd_sparse_attention");
+  }
+  BoundP bp{};
+  p.words = (nb + 31) / 32; p.bg = blocks->block / 32;
+  unsigned* chosen = blocks->chosen ? blocks->chosen : (unsigned*)((char*)workspace + plan.chosen_at);
+  p.chosen = chosen;
+  bp.t = p;
+  bp.summaries = blocks->summaries; bp.tiles = (nb + 63) / 64;
+  bp.block = blocks->block; bp.first = blocks->first; bp.recent = blocks->recent; bp.top = blocks->top;
+  bp.added = blocks->added; bp.score = (double*)((char*)workspace + plan.score_at); bp.chosen = chosen;
+  const dim3 grid(bp.tiles, p.kv, B);
+  const int D = c->head_dim;
+  if (cache_grouped(*c)) {
+    if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, bp);
+    else hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 128, true>), grid, dim3(256), 0, s, bp);
+  } else if (c->dtype == BPD_BF16) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 16, false>), grid, dim3(256), 0, s, bp);
+  else if (D == 16) hipLaunchKernelGGL((block_bounds_kernel<float, 16, false>), grid, dim3(256), 0, s, bp);
+  else if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<float, 64, false>), grid, dim3(256), 0, s, bp);
+  else hipLaunchKernelGGL((block_bounds_kernel<float, 128, false>), grid, dim3(256), 0, s, bp);
+  hipLaunchKernelGGL(block_pick_kernel, dim3(T, p.kv, B), dim3(PICK_T), 0, s, bp);
+  attend<true>(*c, p, plan, s);
+  return launched("bpd_sparse_attention");
+}
+
+int bpd_tree_accept(const int32_t* parent, const int32_t* token, const int32_t* expect, const int32_t* best, const int32_t* length, const int32_t* room, int eos_id,
+                    int B, int T, int32_t* path, int32_t* accepted, int32_t* next, int32_t* new_length, const bpd_cache* c, void* hip_stream) {
+  if (B < 0 || B > 65535 || T < 0 || T > BPD_TREE_MAX) return refuse(BPD_E_ARG, "bpd_tree_accept: B outside 0..65535, or T outside 0..BPD_TREE_MAX");
+  if (c) {
+    if (const char* w = cache_wrong(c)) return refuse(BPD_E_ARG, w);
+    if (B > c->max_batch) return refuse(BPD_E_ARG, "bpd_tree_accept: B over max_batch");
+    if (c->n_layers > 65535) return refuse(BPD_E_CAPACITY, "bpd_tree_accept: more than 65535 layers");
+  }
+  if (B == 0) return BPD_OK;
+  if (!expect || !length || !accepted || !next || !new_length || (T > 0 && (!parent || !token || !best || !path))) return refuse(BPD_E_ARG, "bpd_tree_accept: null argument");
+  // (every workgroup reads the inputs, one writes the results)
+  const struct { const void* p; size_t n; } in[] = {{parent, (size_t)B * T}, {token, (size_t)B * T}, {best, (size_t)B * T}, {expect, (size_t)B}, {length, (size_t)B}, {room, room ? (size_t)B : 0}};
+  const struct { const void* p; size_t n; } res[] = {{path, (size_t)B * T}, {accepted, (size_t)B}, {next, (size_t)B}, {new_length, (size_t)B}};
+  for (const auto& r : res)
+    for (const auto& i : in)
+      if (i.n && r.n && (const char*)r.p < (const char*)i.p + 4 * i.n && (const char*)i.p < (const char*)r.p + 4 * r.n) return refuse(BPD_E_ARG, "bpd_tree_accept: results overlap what is read");
+  AcceptP p{parent, token, expect, best, length, room, path, accepted, next, new_length, eos_id, T, B, nullptr, nullptr, 0, 1, 0};
+  const hipStream_t s = (hipStream_t)hip_stream;
+  dim3 grid(1, 1, B);
+  int D = 64;
+  bool f32 = false, grouped = true;
+  if (c) {
+    p.K = c->k; p.V = c->v; p.layer = (long)cache_layer_elements(*c); p.kv = c->n_kv_heads; p.cap = c->capacity;
+    grid = dim3(c->n_kv_heads, c->n_layers, B);
+    D = c->head_dim; f32 = c->dtype == BPD_F32; grouped = cache_grouped(*c);
+  }
+  if (grouped) {
+    if (D == 64) hipLaunchKernelGGL((tree_accept_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((tree_accept_kernel<bf16_t, 128, true>), grid, dim3(256), 0, s, p);
+  } else if (!f32) hipLaunchKernelGGL((tree_accept_kernel<bf16_t, 16, false>), grid, dim3(256), 0, s, p);
+  else if (D == 16) hipLaunchKernelGGL((tree_accept_kernel<float, 16, false>), grid, dim3(256), 0, s, p);
+  else if (D == 64) hipLaunchKernelGGL((tree_accept_kernel<float, 64, false>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tree_accept_kernel<float, 128, false>), grid, dim3(256), 0, s, p);
+  return launched("bpd_tree_accept");
+}
+
+}  // extern "C"

@@ -1,0 +1,422 @@
+// Rows stored into a cache, blocks of it chosen by a bound of their scores, and trees of drafts verified.  Included by bpd_cache.hip after
+// bpd_cache_attention.h.
+#pragma once
+#include "bpd_cache_attention.h"
+
+// Where the element (key, dimension c) lies in a sequence's and head's part of a cache in operand order (c % 8 == 0: eight dimensions of K side by side)
+template <int D> __device__ __forceinline__ size_t k_at(int key, int c) {
+  return (size_t)(key >> 5) * (TREE_GROUP * D) + ((key >> 2) & 1) * (16 * D) + (c >> 5) * 512 + (((c >> 3) & 3) * 16 + ((key >> 3) & 3) * 4 + (key & 3)) * 8 + (c & 7);
+}
+template <int D> __device__ __forceinline__ size_t v_at(int key, int c) {
+  return (size_t)(key >> 5) * (TREE_GROUP * D) + (c >> 4) * 512 + (((key >> 3) & 3) * 16 + (c & 15)) * 8 + (key & 7);
+}
+
+// ------------------------------------------------------------------------------------------------ rows into a cache
+
+struct RowsP { const void* data; int f32, vec; long layer, seq, row, head; };      // vec: eight elements can be loaded at once
+struct StoreP {
+  RowsP k, v;
+  void *K, *V; long layer;                       // elements of a layer's cache
+  int B, T, kv, cap;
+  const int* start; const int* count;            // count null: T
+};
+__device__ __forceinline__ u32x4 rows_bf16x8(const RowsP& p, long at) {
+  if (!p.f32) {
+    const bf16_t* s = (const bf16_t*)p.data + at;
+    if (p.vec) return *(const u32x4*)s;
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (unsigned)s[2 * j] | (unsigned)s[2 * j + 1] << 16;
+    return w;
+  }
+  const float* s = (const float*)p.data + at;
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = cvt_pk_bf16(s[2 * j], s[2 * j + 1]);
+  return w;
+}
+// Which rows of sequence b's part go where: row i to key first + i, for lo <= i < hi
+__device__ __forceinline__ void store_extent(const StoreP& p, int b, int& first, int& lo, int& hi) {
+  first = p.start[b];
+  int n = p.count ? p.count[b] : p.T;
+  n = n < 0 ? 0 : (n > p.T ? p.T : n);
+  lo = 0;
+  hi = first < 0 || first >= p.cap ? 0 : (n < p.cap - first ? n : p.cap - first);
+}
+// One group of 32 keys of one (layer, sequence, head) per workgroup.  A stream in and a stream out: K goes by 16-byte pieces straight to its place; V, of which eight
+// keys of a dimension lie side by side, is turned in LDS.  Pieces that only some of the new rows are in keep the others.
+template <int D>
+__global__ __launch_bounds__(256) void store_groups_kernel(StoreP p) {
+  constexpr int PIECES = 4 * D;                  // of 8 elements, in a group of K, and in one of V
+  __shared__ __attribute__((aligned(16))) bf16_t v_s[32][D + 8];
+  const int tid = threadIdx.x, h = blockIdx.y, layer = blockIdx.z / p.B, b = blockIdx.z - layer * p.B;
+  int first, lo, hi;
+  store_extent(p, b, first, lo, hi);
+  if (hi <= lo) return;
+  const int key0 = ((first >> 5) + (int)blockIdx.x) * 32;
+  if (key0 >= first + hi) return;
+  const long ks = (long)layer * p.k.layer + (long)b * p.k.seq + (long)h * p.k.head, vs = (long)layer * p.v.layer + (long)b * p.v.seq + (long)h * p.v.head;
+  const size_t part = (size_t)layer * p.layer + ((size_t)b * p.kv + h) * p.cap * D + (size_t)key0 * D;
+  bf16_t *K = (bf16_t*)p.K + part, *V = (bf16_t*)p.V + part;
+  for (int x = tid; x < PIECES; x += 256) {      // V's rows: D / 8 pieces each
+    const int key = x / (D / 8), c = x % (D / 8) * 8, i = key0 + key - first;
+    u32x4 w = u32x4{0, 0, 0, 0};
+    if (i >= lo && i < hi) w = rows_bf16x8(p.v, vs + (long)i * p.v.row + c);
+    *(u32x4*)&v_s[key][c] = w;
+  }
+  for (int x = tid; x < PIECES; x += 256) {      // [t][s][q][a][r]
+    const int r = x & 3, a = (x >> 2) & 3, q = (x >> 4) & 3, s = (x >> 6) % (D / 32), t = (x >> 6) / (D / 32), i = key0 + 8 * a + 4 * t + r - first;
+    if (i >= lo && i < hi) *(u32x4*)(K + x * 8) = rows_bf16x8(p.k, ks + (long)i * p.k.row + 32 * s + 8 * q);
+  }
+  __syncthreads();
+  for (int x = tid; x < PIECES; x += 256) {      // [tile][q][c]
+    const int c = x & 15, q = (x >> 4) & 3, t = x >> 6, i = key0 + 8 * q - first;
+    bf16_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = v_s[8 * q + j][16 * t + c];
+    if (i >= lo && i + 7 < hi) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = (unsigned)e[2 * j] | (unsigned)e[2 * j + 1] << 16;
+      *(u32x4*)(V + x * 8) = w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) if (i + j >= lo && i + j < hi) V[x * 8 + j] = e[j];
+    }
+  }
+}
+// Caches whose rows lie as they are: an element per thread
+template <typename S>
+__global__ __launch_bounds__(256) void store_rows_kernel(StoreP p, int D) {
+  const int layer = blockIdx.z / p.B, b = blockIdx.z - layer * p.B, i = blockIdx.x;
+  int first, lo, hi;
+  store_extent(p, b, first, lo, hi);
+  if (i < lo || i >= hi) return;
+  for (int x = threadIdx.x; x < p.kv * D; x += 256) {
+    const int h = x / D, c = x - h * D;
+    const size_t to = (size_t)layer * p.layer + ((size_t)b * p.cap + first + i) * p.kv * D + x;
+    const long ka = (long)layer * p.k.layer + (long)b * p.k.seq + (long)i * p.k.row + (long)h * p.k.head + c, va = (long)layer * p.v.layer + (long)b * p.v.seq + (long)i * p.v.row + (long)h * p.v.head + c;
+    ((S*)p.K)[to] = from_f<S>(p.k.f32 ? ((const float*)p.k.data)[ka] : bf2f(((const bf16_t*)p.k.data)[ka]));
+    ((S*)p.V)[to] = from_f<S>(p.v.f32 ? ((const float*)p.v.data)[va] : bf2f(((const bf16_t*)p.v.data)[va]));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ blocks chosen by a bound
+
+// Summaries: per (sequence, key head) tiles of 64 blocks, [2: smallest, largest][D / 8][64 blocks][8], so that a wave with a block per lane reads 1 KiB at a time.
+struct BoundP {
+  TreeP t;
+  void* summaries; int tiles;                    // 64 blocks each
+  int block, first, recent, top;
+  const int* added;                              // rows behind which the summaries are still those of the last call (null: all are made anew)
+  double* score;                                 // [b][kv head][node][64 tiles]
+  unsigned* chosen;                              // [b][kv head][node][words]
+};
+// Upper bound of a group's scores in a block, summed over its G heads:  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
+// the heads are added first and cost nothing.  In 64 bits: products of bf16 numbers and their sums are then as good as exact, and which blocks are chosen does not
+// depend on an order of summation.  (2 D multiply-adds per block and node, an eighth of those of 32 keys with G = 2: 1 .. 2 us.)
+// One tile of 64 blocks of one (sequence, key head) per workgroup: a block per lane, the waves share the dimensions and meet in LDS.
+template <typename S, int D, bool GROUPED>
+__global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
+  constexpr int RC = 8, PART = D / 4;            // nodes at a time; dimensions per wave
+  constexpr int BYTES = RC * 2 * D * 8 > 4096 * (int)sizeof(S) ? RC * 2 * D * 8 : 4096 * (int)sizeof(S);
+  __shared__ __attribute__((aligned(16))) unsigned char buf_s[BYTES];
+  double (*q_s)[2][D] = (double (*)[2][D])buf_s;                        // sums over the group of the positive and of the negative parts
+  __shared__ double sum_s[4][RC][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), tile = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  int len, there;
+  tree_extent(p.t, b, len, there);
+  const int done = len / p.block, blk0 = 64 * tile;
+  if (blk0 >= done) return;
+  S* sum = (S*)p.summaries + (((size_t)b * p.t.kv + hk) * p.tiles + tile) * (2 * D * 64);
+  // blocks that the last rows have touched
+  int from = 0;
+  if (p.added) { const int n = p.added[b]; from = n < 0 ? done : (n >= len ? 0 : (len - n) / p.block); }
+  const int f0 = max(from, blk0), f1 = min(done, blk0 + 64);
+  for (int blk = f0; blk < f1; ++blk) {
+    // (a thread has eight, or one, dimensions of some of the rows: the threads meet in LDS)
+    S* lo_s = (S*)buf_s;                         // [256 / (D / 8)][D] smallest, then as many largest
+    constexpr int W = D / 8, PER = 256 / W;
+    const int w = tid % W, rr = tid / W;
+    float mn[8], mx[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { mn[j] = INFINITY; mx[j] = -INFINITY; }
+    for (int r = rr; r < p.block; r += PER) {
+      const int key = blk * p.block + r;
+      const S* k;
+      if constexpr (GROUPED) k = (const S*)p.t.K + ((size_t)b * p.t.kv + hk) * p.t.cap * D + k_at<D>(key, 8 * w);
+      else k = (const S*)p.t.K + ((size_t)b * p.t.cap + key) * p.t.kv * D + (size_t)hk * D + 8 * w;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { const float v = to_f<S>(k[j]); mn[j] = fminf(mn[j], v); mx[j] = fmaxf(mx[j], v); }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { lo_s[rr * D + 8 * w + j] = from_f<S>(mn[j]); lo_s[(PER + rr) * D + 8 * w + j] = from_f<S>(mx[j]); }
+    __syncthreads();
+    if (tid < 2 * W) {
+      const int big = tid / W, c = tid % W * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v = to_f<S>(lo_s[big * PER * D + c + j]);
+        for (int r = 1; r < PER && r < p.block; ++r) { const float u = to_f<S>(lo_s[(big * PER + r) * D + c + j]); v = big ? fmaxf(v, u) : fminf(v, u); }
+        sum[((size_t)(big * W + c / 8) * 64 + blk - blk0) * 8 + j] = from_f<S>(v);
+      }
+    }
+    __syncthreads();
+  }
+  if (f1 > f0) { __threadfence_block(); __syncthreads(); }
+  const TreeP& t = p.t;
+  for (int n0 = 0; n0 < t.T; n0 += RC) {
+    const int nn = min(RC, t.T - n0);
+    for (int x = tid; x < nn * D; x += 256) {
+      const int n = x / D, c = x - n * D;
+      double pos = 0, neg = 0;
+      for (int g = 0; g < t.G; ++g) {
+        const long at = (long)b * t.q_seq + (long)(n0 + n) * t.q_row + (long)(hk * t.G + g) * t.q_head + c;
+        const float v = t.q_f32 ? ((const float*)t.q)[at] : bf2f(((const bf16_t*)t.q)[at]);
+        pos += v > 0.f ? (double)v : 0.0;
+        neg += v < 0.f ? (double)v : 0.0;
+        if (v != v) pos = neg = (double)v;
+      }
+      q_s[n][0][c] = pos; q_s[n][1][c] = neg;
+    }
+    __syncthreads();
+    double acc[RC];
+#pragma unroll
+    for (int n = 0; n < RC; ++n) acc[n] = 0;
+    for (int c = wave * PART; c < (wave + 1) * PART; c += 4) {
+      float mn[4], mx[4];
+      const S* a = sum + ((size_t)(c / 8) * 64 + lane) * 8 + (c & 7);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { mn[j] = to_f<S>(a[j]); mx[j] = to_f<S>(a[D * 64 + j]); }
+#pragma unroll
+      for (int n = 0; n < RC; ++n) {
+        if (n >= nn) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { acc[n] = fma(q_s[n][0][c + j], (double)mx[j], acc[n]); acc[n] = fma(q_s[n][1][c + j], (double)mn[j], acc[n]); }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < RC; ++n) if (n < nn) sum_s[wave][n][lane] = acc[n];
+    __syncthreads();
+    for (int x = tid; x < nn * 64; x += 256) {
+      const int n = x >> 6, l = x & 63;
+      p.score[((((size_t)b * t.kv + hk) * t.T + n0 + n) * p.tiles + tile) * 64 + l] = (sum_s[0][n][l] + sum_s[1][n][l]) + (sum_s[2][n][l] + sum_s[3][n][l]);
+    }
+    __syncthreads();
+  }
+}
+
+// The blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the lower block; a bound that
+// is no number comes last.  Order-preserving 64-bit keys; a digit of eight bits at a time from the first bit in which they differ (most keys share sign and exponent,
+// and a histogram of those would be one counter), until the digit that the last chosen one is in holds no more than are wanted.
+constexpr int PICK_T = 512, PICK_N = TREE_BLOCKS_MAX / PICK_T;
+__global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
+  __shared__ unsigned hist[256];
+  __shared__ unsigned long long and_s[PICK_T / 64], or_s[PICK_T / 64];
+  __shared__ int cnt_s[PICK_N][PICK_T / 64];
+  __shared__ int digit_s, need_s, left_s;
+  __shared__ mask64 ok_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  const TreeP& t = p.t;
+  int len, there;
+  tree_extent(t, b, len, there);
+  if (wave == 0) {
+    mask64 anc; bool ok;
+    tree_ancestors(t.parent ? t.parent + (long)b * t.T : nullptr, t.T, there, lane, anc, ok);
+    const mask64 all = __ballot(ok);
+    if (lane == 0) ok_s = all;
+  }
+  const int done = len / p.block, lo = min(p.first, done), hi = max(lo, done - p.recent), words = t.words;
+  unsigned* out = p.chosen + (((size_t)b * t.kv + hk) * t.T + n) * words;
+  __syncthreads();
+  const bool there_n = ok_s >> n & 1;
+  const int cand = hi - lo, take = there_n ? min(p.top, cand) : 0;
+  const bool everything = take == cand;
+  unsigned long long key[PICK_N];
+  unsigned long long thr = 0;
+  int need = 0;                                  // of the keys that equal thr, so many of the lowest blocks
+  if (!everything && take > 0) {
+    const double* score = p.score + (((size_t)b * t.kv + hk) * t.T + n) * p.tiles * 64;
+    unsigned long long a = ~0ull, o = 0ull;
+#pragma unroll
+    for (int j = 0; j < PICK_N; ++j) {
+      const int blk = j * PICK_T + tid;
+      key[j] = 0;
+      if (blk >= lo && blk < hi) {
+        const double s = score[blk] + 0.0;       // (no negative zero)
+        const unsigned long long u = (unsigned long long)__double_as_longlong(s);
+        key[j] = s != s ? 1ull : (u >> 63 ? ~u : u | 1ull << 63);
+        a &= key[j]; o |= key[j];
+      }
+    }
+    for (int x = 32; x > 0; x >>= 1) { a &= __shfl_xor(a, x, 64); o |= __shfl_xor(o, x, 64); }
+    if (lane == 0) { and_s[wave] = a; or_s[wave] = o; }
+    __syncthreads();
+    for (int w = 0; w < PICK_T / 64; ++w) { a &= and_s[w]; o |= or_s[w]; }
+    const unsigned long long differ = a ^ o;
+    need = take;
+    int top_bit = differ ? 64 - __clzll((long long)differ) : 0;        // bits from here on up are the same in all
+    thr = top_bit < 64 ? a >> top_bit << top_bit : 0ull;
+    while (top_bit > 0) {
+      const int bits = min(8, top_bit), sh = top_bit - bits;
+      for (int x = tid; x < 256; x += PICK_T) hist[x] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < PICK_N; ++j) {
+        const int blk = j * PICK_T + tid;
+        if (blk >= lo && blk < hi && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit)) atomicAdd(&hist[(key[j] >> sh) & ((1u << bits) - 1)], 1u);
+      }
+      __syncthreads();
+      if (wave == 0) {                           // from the largest digit down: the first at which `need` are reached
+        const int d0 = 255 - 4 * lane;
+        unsigned c[4], mine = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { c[j] = hist[d0 - j]; mine += c[j]; }
+        unsigned upto = mine;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) { const unsigned v = __shfl_up(upto, x, 64); if (lane >= x) upto += v; }
+        unsigned before = upto - mine;
+        if (before < (unsigned)need && upto >= (unsigned)need) {
+          int d = d0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (before + c[j] >= (unsigned)need) { d = d0 - j; left_s = (int)c[j]; break; }
+            before += c[j];
+          }
+          digit_s = d; need_s = need - (int)before;
+        }
+      }
+      __syncthreads();
+      thr |= (unsigned long long)digit_s << sh;
+      need = need_s;
+      top_bit = sh;
+      const bool all_of_it = left_s == need;
+      __syncthreads();
+      if (all_of_it) break;                      // (thr's lower bits are zero: every key with these upper ones is at least that)
+    }
+    // ties: `need` keys of those whose upper bits are thr's, the lowest blocks
+#pragma unroll
+    for (int j = 0; j < PICK_N; ++j) {
+      const int blk = j * PICK_T + tid;
+      const bool same = blk >= lo && blk < hi && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit);
+      const mask64 m = __ballot(same);
+      if (lane == 0) cnt_s[j][wave] = __popcll(m);
+    }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int j = 0; j < PICK_N; ++j) {
+      const int blk = j * PICK_T + tid;
+      const bool in = blk >= lo && blk < hi;
+      const bool same = in && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit);
+      const bool above = in && top_bit < 64 && key[j] >> top_bit > thr >> top_bit;
+      int at = before;
+      for (int w = 0; w < PICK_T / 64; ++w) { if (w < wave) at += cnt_s[j][w]; before += cnt_s[j][w]; }
+      const mask64 m = __ballot(same);
+      const int mine = at + __popcll(m & ((1ull << lane) - 1));
+      key[j] = above || (same && mine < need);   // (from here on: whether it is chosen)
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < PICK_N; ++j) {
+    const int blk = j * PICK_T + tid;
+    const bool mid = blk >= lo && blk < hi && (everything || (take > 0 && key[j]));
+    const bool pick = there_n && blk < done && (blk < lo || blk >= hi || mid);
+    const mask64 m = __ballot(pick);
+    const int w = (j * PICK_T + wave * 64) / 32;
+    if (lane < 2 && w + lane < words) out[w + lane] = (unsigned)(m >> (32 * lane));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ trees verified
+
+struct AcceptP {
+  const int *parent, *token, *expect, *best, *length, *room;
+  int *path, *accepted, *next, *new_length;
+  int eos, T, B;
+  void *K, *V; long layer; int kv, cap;          // K null: no rows to move
+};
+// The longest path of nodes that p_1 agrees with: from the prefix down, each time the first child of the last accepted node whose token is the one that is wanted there.
+// Cut behind the first EOS and at `room`; nodes whose rows are past the cache's end are absent.  By one wave, a node per lane; every workgroup finds it again (some 100 cycles per accepted node, less than a
+// second launch), and moves the rows of one layer's (sequence, head) that the path skipped to: read as a whole, then written.
+__device__ __forceinline__ int accept_walk(const AcceptP& p, int b, int lane, int& node, int& next) {
+  const int T = p.T, par = lane < T ? p.parent[(long)b * T + lane] : -2, tok = lane < T ? p.token[(long)b * T + lane] : 0, bst = lane < T ? p.best[(long)b * T + lane] : 0;
+  int want = p.expect[b], cur = -1, n = 0, most = T;
+  const int len = p.length[b], there = p.K ? min(T, p.cap - len) : T;
+  if (p.room) most = min(most, p.room[b]);
+  if (len < 0) most = 0;
+  node = -1;
+  while (n < most) {
+    const mask64 m = __ballot(lane > cur && lane < there && par == cur && tok == want);
+    if (!m) break;
+    cur = __ffsll((long long)m) - 1;
+    if (lane == n) node = cur;
+    ++n;
+    want = __shfl(bst, cur, 64);
+    if (p.eos >= 0 && __shfl(tok, cur, 64) == p.eos) break;
+  }
+  next = want;
+  return n;
+}
+template <typename S, int D, bool GROUPED>
+__global__ __launch_bounds__(256) void tree_accept_kernel(AcceptP p) {
+  __shared__ int path_s[TREE_MAX];
+  __shared__ int n_s;
+  const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x, layer = blockIdx.y, b = blockIdx.z;
+  const int len = p.length[b];
+  if (tid < 64) {
+    int node, next;
+    const int n = accept_walk(p, b, lane, node, next);
+    path_s[lane] = node;
+    if (lane == 0) n_s = n;
+    if (h == 0 && layer == 0) {
+      if (lane < p.T) p.path[(long)b * p.T + lane] = node;
+      if (lane == 0) { p.accepted[b] = n; p.next[b] = next; p.new_length[b] = len + n; }
+    }
+  }
+  __syncthreads();
+  const int n = n_s;
+  if (!p.K || n == 0 || path_s[n - 1] == n - 1) return;          // (nodes come in order: then none has moved)
+  S *K = (S*)p.K + (size_t)layer * p.layer, *V = (S*)p.V + (size_t)layer * p.layer;
+  if constexpr (GROUPED) {
+    K += ((size_t)b * p.kv + h) * p.cap * D; V += ((size_t)b * p.kv + h) * p.cap * D;
+    constexpr int KP = TREE_MAX * D / 8 / 256, VP = TREE_MAX * D / 256;
+    u32x4 k[KP]; S v[VP];
+#pragma unroll
+    for (int x = 0; x < KP; ++x) {
+      const int e = x * 256 + tid, m = e / (D / 8), c = e % (D / 8) * 8;
+      if (m < n && path_s[m] != m) k[x] = *(const u32x4*)(K + k_at<D>(len + path_s[m], c));
+    }
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = e / D, c = e % D;
+      if (m < n && path_s[m] != m) v[x] = V[v_at<D>(len + path_s[m], c)];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < KP; ++x) {
+      const int e = x * 256 + tid, m = e / (D / 8), c = e % (D / 8) * 8;
+      if (m < n && path_s[m] != m) *(u32x4*)(K + k_at<D>(len + m, c)) = k[x];
+    }
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = e / D, c = e % D;
+      if (m < n && path_s[m] != m) V[v_at<D>(len + m, c)] = v[x];
+    }
+  } else {
+    constexpr int VP = (TREE_MAX * D + 255) / 256;
+    S k[VP], v[VP];
+    const size_t at = ((size_t)b * p.cap + len) * p.kv * D + (size_t)h * D;
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = e / D, c = e % D;
+      if (m < n && path_s[m] != m) { const size_t s = at + (size_t)path_s[m] * p.kv * D + c; k[x] = K[s]; v[x] = V[s]; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = e / D, c = e % D;
+      if (m < n && path_s[m] != m) { const size_t s = at + (size_t)m * p.kv * D + c; K[s] = k[x]; V[s] = v[x]; }
+    }
+  }
+}
