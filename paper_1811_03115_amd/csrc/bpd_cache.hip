@@ -46,39 +46,52 @@ const char* rows_wrong(const bpd_rows* r) {
 }
 RowsP rows_of(const bpd_rows& r) { return RowsP{r.data, r.dtype == BPD_F32, rows_aligned(r) ? 1 : 0, (long)r.layer, (long)r.seq, (long)r.row, (long)r.head}; }
 
-template <int D, int MT, bool SPARSE>
-void attend_groups(const TreeP& p, dim3 grid, hipStream_t s) {
-  if (p.q_f32) hipLaunchKernelGGL((tree_attention_kernel<D, MT, true, SPARSE>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((tree_attention_kernel<D, MT, false, SPARSE>), grid, dim3(256), 0, s, p);
+template <int D, int MT, int NW, bool SPARSE>
+void attend_few(const TreeP& p, hipStream_t s) {
+  const dim3 grid(p.nsplit, p.kv, p.B);
+  if constexpr (MT <= 2) {                       // (queries of fp32 and of many rows take other tiles: attend_groups)
+    if (p.q_f32) { hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, true, SPARSE>), grid, dim3(64 * NW), 0, s, p); return; }
+  }
+  hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, false, SPARSE>), grid, dim3(64 * NW), 0, s, p);
 }
 template <int D, bool SPARSE>
-void attend_tiles(const TreeP& p, int mt, dim3 grid, hipStream_t s) {
-  if (mt == 1) attend_groups<D, 1, SPARSE>(p, grid, s);
-  else if (mt == 2) attend_groups<D, 2, SPARSE>(p, grid, s);
-  else if constexpr (D == 64) attend_groups<D, 4, SPARSE>(p, grid, s);
+void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
+  const int R = p.T * p.G;
+  if (plan.rows || (p.q_f32 && R > 32)) {
+    if (p.q_f32) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 8, true, SPARSE>), dim3(p.nsplit * ((R + 127) / 128), p.kv, p.B), dim3(512), 0, s, p);
+    else if (plan.waves == 4) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.nsplit * plan.blocks, p.kv, p.B), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 8, false, SPARSE>), dim3(p.nsplit * plan.blocks, p.kv, p.B), dim3(512), 0, s, p);
+  } else if (plan.mt == 1) {
+    if (plan.waves == 4) attend_few<D, 1, 4, SPARSE>(p, s);
+    else attend_few<D, 1, 8, SPARSE>(p, s);
+  } else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
+  else if (plan.mt == 3) attend_few<D, 3, 4, SPARSE>(p, s);
+  else attend_few<D, 4, 4, SPARSE>(p, s);
+}
+template <int D, int NG>
+void join_of(const TreeP& p, hipStream_t s) {
+  const long rows = (long)p.B * p.kv * p.T * p.G, per = 256 / (D / 4 * NG);
+  hipLaunchKernelGGL((tree_join_kernel<D, NG>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, p);
+}
+template <int D>
+void join(const TreeP& p, hipStream_t s) {       // (threads for every fourth, or eighth, split)
+  if (p.nsplit <= 4) join_of<D, 1>(p, s);
+  else if (p.nsplit <= 16) join_of<D, 4>(p, s);
+  else join_of<D, 8>(p, s);
 }
 template <bool SPARSE>
 void attend(const bpd_cache& c, const TreeP& p, const TreePlan& plan, hipStream_t s) {
-  const dim3 grid(p.kv * p.nsplit, plan.blocks, p.B);
   const int D = c.head_dim;
   if (cache_grouped(c)) {
-    if (D == 64) attend_tiles<64, SPARSE>(p, plan.mt, grid, s); else attend_tiles<128, SPARSE>(p, plan.mt, grid, s);
-  } else if (c.dtype == BPD_BF16) {
-    hipLaunchKernelGGL((tree_rows_kernel<bf16_t, 16, SPARSE>), grid, dim3(256), 0, s, p);
-  } else if (D == 16) {
-    hipLaunchKernelGGL((tree_rows_kernel<float, 16, SPARSE>), grid, dim3(256), 0, s, p);
-  } else if (D == 64) {
-    hipLaunchKernelGGL((tree_rows_kernel<float, 64, SPARSE>), grid, dim3(256), 0, s, p);
+    if (D == 64) attend_groups<64, SPARSE>(p, plan, s); else attend_groups<128, SPARSE>(p, plan, s);
   } else {
-    hipLaunchKernelGGL((tree_rows_kernel<float, 128, SPARSE>), grid, dim3(256), 0, s, p);
+    const dim3 grid(p.nsplit * plan.blocks, p.kv, p.B);
+    if (c.dtype == BPD_BF16) hipLaunchKernelGGL((tree_rows_kernel<bf16_t, 16, SPARSE>), grid, dim3(256), 0, s, p);
+    else if (D == 16) hipLaunchKernelGGL((tree_rows_kernel<float, 16, SPARSE>), grid, dim3(256), 0, s, p);
+    else if (D == 64) hipLaunchKernelGGL((tree_rows_kernel<float, 64, SPARSE>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((tree_rows_kernel<float, 128, SPARSE>), grid, dim3(256), 0, s, p);
   }
-  if (p.nsplit > 1) {
-    const long rows = (long)p.B * p.kv * p.T * p.G;
-    const int per = 256 / (D / 4), n = (int)((rows + per - 1) / per);
-    if (D == 16) hipLaunchKernelGGL(tree_join_kernel<16>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
-    else if (D == 64) hipLaunchKernelGGL(tree_join_kernel<64>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
-    else hipLaunchKernelGGL(tree_join_kernel<128>, dim3(n), dim3(256), 0, s, p, 16 * plan.mt);
-  }
+  if (p.nsplit > 1) { if (D == 16) join<16>(p, s); else if (D == 64) join<64>(p, s); else join<128>(p, s); }
 }
 
 // What bpd_tree_attention and bpd_sparse_attention check alike; null: nothing is wrong
@@ -100,7 +113,8 @@ TreeP attention_args(const bpd_cache& c, const bpd_rows& q, const bpd_rows& out,
   p.K = c.k; p.V = c.v;
   p.B = B; p.T = T; p.H = heads; p.kv = c.n_kv_heads; p.G = heads / c.n_kv_heads; p.cap = c.capacity;
   p.length = length; p.parent = parent;
-  p.scale = scale * 1.44269504088896340736f;
+  p.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504088896340736f;
+  p.sign = scale > 0.f ? 1.f : (scale < 0.f ? -1.f : 0.f);
   p.q_f32 = q.dtype == BPD_F32; p.o_f32 = out.dtype == BPD_F32;
   p.vec = rows_aligned(q) && rows_aligned(out);
   return p;

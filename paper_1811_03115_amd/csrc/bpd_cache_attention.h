@@ -21,8 +21,8 @@ struct TreeP {
   const void *K, *V;                             // one layer's cache
   int B, T, H, kv, G, cap;                       // cap: rows per sequence
   const int* length; const int* parent;          // parent null: a chain
-  float scale;                                   // times log2(e)
-  int nsplit; float* part;                       // partial results [b][kv head][row block][split][rows x (D + 2)]
+  float scale, sign;                             // |scale| log2(e) (1 for a scale of 0), and the scale's sign (0)
+  int nsplit; float* part;                       // parts of the keys, and their results
   int q_f32, o_f32, vec;                         // vec: rows of q and out are 16-byte aligned
   // chosen blocks (null: the whole prefix): bits [b][kv head][node][words], blocks of `bg` groups of 32 keys
   const unsigned* chosen; int words, bg;
@@ -147,134 +147,75 @@ __device__ __forceinline__ int tree_list(const unsigned* chosen, int words, int 
   return all;
 }
 
-// bf16 heads of D = 64 or 128 in operand order (groups of 32 keys, D x 32 elements of K and as many of V, bpd_attention.h for D = 64; the same with
-// D / 32 steps of K and D / 16 tiles of V otherwise): every operand is one 1 KiB load, nothing of K and V goes through LDS.
-// A workgroup has 16 MT rows of one (sequence, key head) and every nsplit-th part of its items; its four waves split those by single items, each with its own
-// maximum, sum and results, and meet once in LDS.
-//   scores^T = K Q^T       32 keys x 16 rows per item and row tile
-//   softmax                in the lane, then across the four lanes of a row
+// What a wave does with one item (32 keys) for its MT row tiles, keys and values being operands in registers.
+//   scores^T = K Q^T       32 keys x 16 rows per tile
+//   softmax                p = 2^(s scale - m); m is raised, and sums and results with it, only when a score passes it by 2^8 (fp32 has room for that; nothing is rounded by
+//                          it): maxima over the four lanes of a row, and multiplications of all results, are then rare.  Sums stay in their lanes until the end.
 //   out^T += V^T P^T       the probabilities as they lie are the second operand
-// Queries of bf16 are exact, those of fp32 a pair; the scale is applied to the fp32 scores.  Probabilities go in as a pair hi + lo: as single bf16 numbers their rounding
-// adds as much error as that of the bf16 results (sum over keys of p (1 +- 2^-9) v), which the pair's second product takes to 2^-17.
-template <int D, int MT, bool QF32, bool SPARSE>
-__global__ __launch_bounds__(256) void tree_attention_kernel(TreeP p) {
-  constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D;
-  __shared__ __attribute__((aligned(16))) f32x4 o_s[4][VT][64];
-  __shared__ float m_s[4][MT * 16], l_s[4][MT * 16];
-  __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
-  __shared__ int sums_s[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
-  const int split = blockIdx.x % p.nsplit, hk = blockIdx.x / p.nsplit, rb = blockIdx.y, b = blockIdx.z;
-  const int R = p.T * p.G, r0 = rb * 16 * MT;
-  int len, there;
-  tree_extent(p, b, len, there);
-  const int* parent = p.parent ? p.parent + (long)b * p.T : nullptr;
-  mask64 anc; bool ok;
-  tree_ancestors(parent, p.T, there, lane, anc, ok);
-  const mask64 present = __ballot(ok);
-  // this lane's rows
-  mask64 seen[MT]; int node[MT]; bool row_ok[MT];
-  bf16x8 qh[MT][KS], ql[QF32 ? MT : 1][KS];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int r = r0 + 16 * t + lr, n = r < R ? r / p.G : 0;
-    node[t] = n;
-    seen[t] = (mask64)(unsigned)__shfl((int)(anc >> 32), n, 64) << 32 | (unsigned)__shfl((int)anc, n, 64);
-    row_ok[t] = r < R && seen[t] != 0;
-    if (r >= R) seen[t] = 0;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      float v[8] = {};
-      if (row_ok[t]) tree_q8(p, b, n, hk * p.G + r - n * p.G, 32 * s + 8 * lq, v);
-      bf16x8 lo;
-      tree_pair(v, qh[t][s], lo);
-      if constexpr (QF32) ql[t][s] = lo;
-    }
-  }
-  const int ngr = (len + there + 31) >> 5;
-  TreeItems it{0, 0, ngr, nullptr, 1};
-  const unsigned* picks = nullptr;
-  if constexpr (SPARSE) {
-    picks = p.chosen + ((long)b * p.kv + hk) * p.T * p.words;
-    const int done = len / (32 * p.bg), n0 = r0 / p.G, n1 = min(p.T, (min(R, r0 + 16 * MT) + p.G - 1) / p.G);
-    it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
-    it.listed = tree_list(picks, p.words, n0, n1, done, list_s, sums_s) * p.bg;
-    it.n = it.listed + ngr - it.tail0;
-  }
-  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
-  const bf16_t* Kb = (const bf16_t*)p.K + ((size_t)b * p.kv + hk) * p.cap * D;
-  const bf16_t* Vb = (const bf16_t*)p.V + ((size_t)b * p.kv + hk) * p.cap * D;
-  float m_run[MT], l_run[MT];
-  f32x4 acc[MT][VT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    m_run[t] = -INFINITY; l_run[t] = 0.f;
-#pragma unroll
-    for (int x = 0; x < VT; ++x) acc[t][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  for (int i = i0 + wave; i < i1; i += 4) {
-    const int g = __builtin_amdgcn_readfirstlane(it.group(i));
-    const u32x4* kp = (const u32x4*)(Kb + (size_t)g * GRP) + lane;
-    const u32x4* vp = (const u32x4*)(Vb + (size_t)g * GRP) + lane;
-    u32x4 kf[2 * KS], vf[VT];
-#pragma unroll
-    for (int x = 0; x < 2 * KS; ++x) kf[x] = kp[x * 64];
-#pragma unroll
-    for (int x = 0; x < VT; ++x) vf[x] = vp[x * 64];
-    const int at = 32 * g + 8 * lq - len;        // this lane's first key among the drafts
-    const bool edge = 32 * g + 32 > len;         // (the same for the whole wave)
-    if (edge) {                                  // values of rows that nobody sees: their probabilities are zero, their bits unknown
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        unsigned known = 0;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int n = at + 2 * w + e;
-          if (n < 0 || (n < 64 && (present >> n & 1))) known |= 0xFFFFu << (16 * e);
-        }
-#pragma unroll
-        for (int x = 0; x < VT; ++x) vf[x][w] &= known;
-      }
-    }
+// Queries of bf16 are exact, those of fp32 a pair.  Probabilities go in as a pair hi + lo: as single bf16 numbers their rounding adds as much error as that of the bf16
+// results (sum over keys of p (1 +- 2^-9) v), which the pair's second product takes to 2^-17.
+constexpr float TREE_SLACK = 8.f;
+template <int D, int MT, bool QF32>
+struct TreeTiles {
+  static constexpr int KS = D / 32, VT = D / 16;
+  float m[MT], l[MT];                            // per row what is subtracted (base 2; -inf: nothing seen), and this lane's part of the sum
+  f32x4 acc[MT][VT];                             // dimensions 16 x + 4 lq + r of row lr
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      bool vis = row_ok[t];
-      if constexpr (SPARSE) {
-        if (i < it.listed) { const int blk = g / p.bg; vis = vis && (picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1); }
-      }
+      m[t] = -INFINITY; l[t] = 0.f;
+#pragma unroll
+      for (int x = 0; x < VT; ++x) acc[t][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // kf, vf: the item's operands; at: this lane's first key among the drafts; edge: whether any key of the item is a draft (the same for the whole wave); vis: whether
+  // row t sees the item's committed keys; seen: the drafts that it sees; q(t, x): its operand
+  template <typename Q, typename QL>
+  __device__ __forceinline__ void item(const u32x4 (&kf)[2 * KS], const u32x4 (&vf)[VT], int at, bool edge, const bool (&vis)[MT], const mask64 (&seen)[MT], float scale, const Q& q, const QL& ql) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
       f32x4 s[2];
-      float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < KS; ++x) {
           const bf16x8 ka = __builtin_bit_cast(bf16x8, kf[u * KS + x]);
-          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qh[t][x], a, 0, 0, 0);
-          if constexpr (QF32) a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, ql[t][x], a, 0, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int n = at + 4 * u + r;
-          const bool in = !edge || n < 0 ? vis : (n < 64 && (seen[t] >> n & 1));
-          a[r] = in ? a[r] * p.scale : -INFINITY;
-          mx = fmaxf(mx, a[r]);
+          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, q(t, x), a, 0, 0, 0);
+          if constexpr (QF32) a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, ql(t, x), a, 0, 0, 0);
         }
         s[u] = a;
       }
-      mx = max_rows(mx);
-      const float m_new = fmaxf(m_run[t], mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-      float sum = 0.f, pv[8];
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int n = at + 4 * u + r;
+            const bool in = n < 0 ? vis[t] : (n < 64 && (seen[t] >> n & 1));
+            s[u][r] = in ? s[u][r] : -INFINITY;
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[u][r] = vis[t] ? s[u][r] : -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale;
+      if (__any(mx > m[t] + TREE_SLACK)) {
+        mx = max_rows(mx);
+        const float up = fmaxf(m[t], mx), alpha = up == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[t] - up);
+        m[t] = up;
+        l[t] *= alpha;
+#pragma unroll
+        for (int x = 0; x < VT; ++x) acc[t][x] *= alpha;
+      }
+      const float sub = m[t] == -INFINITY ? 0.f : m[t];
+      float pv[8];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) { const float e = __builtin_amdgcn_exp2f(s[u][r] - m_use); pv[4 * u + r] = e; sum += e; }
-      sum = sum_rows(sum);
-      const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m_use);
-      l_run[t] = l_run[t] * alpha + sum;
-      m_run[t] = m_new;
-#pragma unroll
-      for (int x = 0; x < VT; ++x) acc[t][x] *= alpha;
+        for (int r = 0; r < 4; ++r) { const float e = __builtin_amdgcn_exp2f(fmaf(s[u][r], scale, -sub)); pv[4 * u + r] = e; l[t] += e; }
       bf16x8 ph, pl;
       tree_pair(pv, ph, pl);
 #pragma unroll
@@ -285,39 +226,281 @@ __global__ __launch_bounds__(256) void tree_attention_kernel(TreeP p) {
       }
     }
   }
-  // the waves meet
+};
+// Values of rows that nobody sees (behind the drafts, absent nodes): their probabilities are zero, their bits unknown.  at: as above
+template <int VT>
+__device__ __forceinline__ void tree_blank(u32x4 (&vf)[VT], int at, mask64 present) {
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-    if (lq == 0) { m_s[wave][16 * t + lr] = m_run[t]; l_s[wave][16 * t + lr] = l_run[t]; }
-  const long tile0 = (((long)b * p.kv + hk) * gridDim.y + rb) * p.nsplit + split;
-  float* part = p.part + tile0 * (16 * MT) * (D + 2);
+  for (int w = 0; w < 4; ++w) {
+    unsigned known = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int n = at + 2 * w + e;
+      if (n < 0 || (n < 64 && (present >> n & 1))) known |= 0xFFFFu << (16 * e);
+    }
+#pragma unroll
+    for (int x = 0; x < VT; ++x) vf[x][w] &= known;
+  }
+}
+// Row r of a (sequence, key head) pair: its node, what it sees of the drafts, whether it is there
+__device__ __forceinline__ void tree_row(const TreeP& p, int r, int R, mask64 anc, int& node, mask64& seen, bool& ok) {
+  node = r < R ? r / p.G : 0;
+  seen = (mask64)(unsigned)__shfl((int)(anc >> 32), node, 64) << 32 | (unsigned)__shfl((int)anc, node, 64);
+  if (r >= R) seen = 0;
+  ok = seen != 0;
+}
+// Its query's operand for the dimensions 32 x + 8 lq ..; hi and what that leaves
+__device__ __forceinline__ void tree_q_operand(const TreeP& p, int b, int hk, int r, int node, bool ok, int c, bf16x8& hi, bf16x8& lo) {
+  float v[8] = {};
+  if (ok) tree_q8(p, b, node, hk * p.G + r - node * p.G, c, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= p.sign;    // (of the scale: the maximum is that of the products)
+  tree_pair(v, hi, lo);
+}
+// A row's result or partial result: dimensions c .. c + 3.  Partial results: [pair][split][row][D], then [pair][split][row] maxima and as many sums
+__device__ __forceinline__ void tree_finish4(const TreeP& p, int D, long pair, int b, int hk, int split, int r, int R, int node, int c, float M, float L, const f32x4& o) {
+  if (r >= R) return;
+  if (p.nsplit > 1) {
+    const long at = (pair * p.nsplit + split) * R + r, rows = (long)p.B * p.kv * p.nsplit * R;
+    *(f32x4*)(p.part + at * D + c) = o;
+    if (c == 0) { p.part[rows * D + at] = M; p.part[rows * (D + 1) + at] = L; }
+  } else {
+    // (an absent node has seen nothing: L = 0)
+    tree_store4(p, b, node, hk * p.G + r - node * p.G, c, L > 0.f ? o * (1.f / L) : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
+  }
+}
+
+// bf16 heads of D = 64 or 128 in operand order (groups of 32 keys, D x 32 elements of K and as many of V, bpd_attention.h for D = 64; the same with
+// D / 32 steps of K and D / 16 tiles of V otherwise): every operand is one 1 KiB load, nothing of K and V goes through LDS.
+// Up to 64 rows: a workgroup has all of a (sequence, key head) pair's, and one part in nsplit of its items; its NW waves take single items in turn, each with its own
+// maximum, sum and results, and meet once in LDS.  What bounds it is the stream of K and V; the next item's keys are asked for while this one's values are multiplied.
+template <int D, int MT, int NW, bool QF32, bool SPARSE>
+__global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
+  constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D, SLOTS = NW / 2 > 4 ? NW / 2 : 4;
+  constexpr bool Q_LDS = MT * KS > 8 && !QF32;   // queries of many rows: in LDS, for registers
+  __shared__ __attribute__((aligned(16))) f32x4 o_s[SLOTS][VT][64];
+  __shared__ float m_s[NW][MT * 16], l_s[NW][MT * 16];
+  __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
+  __shared__ int sums_s[NW];
+  static_assert(!Q_LDS || MT * KS <= SLOTS * VT, "queries fit where the results meet");
+  u32x4 (*q_s)[KS][64] = (u32x4 (*)[KS][64])&o_s[0][0][0];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
+  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, R = p.T * p.G;
+  const long pair = (long)b * p.kv + hk;
+  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + (size_t)pair * p.cap * D) + lane;
+  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + (size_t)pair * p.cap * D) + lane;
+  u32x4 kf[2 * KS], kn[2 * KS], vf[VT];
+  auto load_k = [&](u32x4 (&k)[2 * KS], int g) {
+#pragma unroll
+    for (int x = 0; x < 2 * KS; ++x) k[x] = Kb[(size_t)g * (GRP / 8) + x * 64];
+  };
+  // with all keys here the first item's keys do not wait for the length
+  if (!SPARSE && p.nsplit == 1) load_k(kf, min(wave, p.cap / 32 - 1));
+  int len, there;
+  tree_extent(p, b, len, there);
+  mask64 anc; bool ok;
+  tree_ancestors(p.parent ? p.parent + (long)b * p.T : nullptr, p.T, there, lane, anc, ok);
+  const mask64 present = __ballot(ok);
+  mask64 seen[MT]; int node[MT]; bool row_ok[MT];
+  bf16x8 qh[Q_LDS ? 1 : MT][KS], ql[QF32 ? MT : 1][KS];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    if (t > 0) __syncthreads();
+    const int r = 16 * t + lr;
+    tree_row(p, r, R, anc, node[t], seen[t], row_ok[t]);
+    if constexpr (Q_LDS) {
+      if (t % NW != wave) continue;
+      bf16x8 lo;
 #pragma unroll
-    for (int x = 0; x < VT; ++x) o_s[wave][x][lane] = acc[t][x];
-    __syncthreads();
-    for (int x = wave; x < VT; x += 4) {
-      float M = -INFINITY, L = 0.f;
+      for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[0][x], lo); q_s[t][x][lane] = __builtin_bit_cast(u32x4, qh[0][x]); }
+    } else {
+      bf16x8 lo;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, m_s[w][16 * t + lr]);
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-      const float M0 = M == -INFINITY ? 0.f : M;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float a = __builtin_amdgcn_exp2f(m_s[w][16 * t + lr] - M0);
-        L = fmaf(l_s[w][16 * t + lr], a, L);
-        o += o_s[w][x][lane] * a;
-      }
-      const int r = r0 + 16 * t + lr;
-      if (p.nsplit > 1) {
-        *(f32x4*)(part + (16 * t + lr) * D + 16 * x + 4 * lq) = o;
-        if (x == wave && wave == 0 && lq == 0) { part[16 * MT * D + 16 * t + lr] = M; part[16 * MT * (D + 1) + 16 * t + lr] = L; }
-      } else if (r < R) {
-        const float inv = 1.f / L;
-        tree_store4(p, b, node[t], hk * p.G + r - node[t] * p.G, 16 * x + 4 * lq, row_ok[t] && L > 0.f ? o * inv : (row_ok[t] && L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
-      }
+      for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[t][x], lo); if constexpr (QF32) ql[t][x] = lo; }
     }
+  }
+  const int ngr = (len + there + 31) >> 5;
+  TreeItems it{0, 0, ngr, nullptr, 1};
+  const unsigned* picks = nullptr;
+  if constexpr (SPARSE) {
+    picks = p.chosen + pair * p.T * p.words;
+    const int done = len / (32 * p.bg);
+    it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
+    it.listed = tree_list(picks, p.words, 0, p.T, done, list_s, sums_s) * p.bg;
+    it.n = it.listed + ngr - it.tail0;
+  }
+  if constexpr (Q_LDS) __syncthreads();
+  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
+  TreeTiles<D, MT, QF32> tiles;
+  tiles.clear();
+  int i = i0 + wave, g = i < i1 ? __builtin_amdgcn_readfirstlane(it.group(i)) : 0;
+  unsigned word[SPARSE ? MT : 1];                // has the row chosen the item's block?
+  auto load_words = [&](int ii, int gg) {
+    if constexpr (SPARSE) {
+      const int blk = gg / p.bg;
+#pragma unroll
+      for (int t = 0; t < MT; ++t) word[t] = ii < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
+    }
+  };
+  if (i < i1) {
+    load_words(i, g);
+    if (SPARSE || p.nsplit > 1) load_k(kf, g);
+  }
+  auto step = [&](u32x4 (&k)[2 * KS], u32x4 (&k_next)[2 * KS]) {
+#pragma unroll
+    for (int x = 0; x < VT; ++x) vf[x] = Vb[(size_t)g * (GRP / 8) + x * 64];
+    bool vis[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && word[t]; }
+    const int next = i + NW, gn = next < i1 ? __builtin_amdgcn_readfirstlane(it.group(next)) : g;
+    if (next < i1) { load_words(next, gn); load_k(k_next, gn); }
+    const int at = 32 * g + 8 * lq - len;
+    const bool edge = 32 * g + 32 > len;
+    if (edge) tree_blank<VT>(vf, at, present);
+    tiles.item(k, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { if constexpr (Q_LDS) return __builtin_bit_cast(bf16x8, q_s[t][x][lane]); else return qh[t][x]; },
+               [&](int t, int x) { return ql[QF32 ? t : 0][x]; });
+    i = next; g = gn;
+  };
+  while (i < i1) {                               // (two sets of keys in turn)
+    step(kf, kn);
+    if (i >= i1) break;
+    step(kn, kf);
+  }
+  // the waves meet: maxima and sums first, then the upper half's results into the lower half's until four are left
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    tiles.l[t] = sum_rows(tiles.l[t]);
+    if (lq == 0) { m_s[wave][16 * t + lr] = tiles.m[t]; l_s[wave][16 * t + lr] = tiles.l[t]; }
+  }
+  __syncthreads();                               // (and the queries have been read)
+  float M[MT], L[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    M[t] = -INFINITY; L[t] = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M[t] = fmaxf(M[t], m_s[w][16 * t + lr]);
+    const float M0 = M[t] == -INFINITY ? 0.f : M[t];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) L[t] = fmaf(l_s[w][16 * t + lr], __builtin_amdgcn_exp2f(m_s[w][16 * t + lr] - M0), L[t]);
+    const float a = __builtin_amdgcn_exp2f(tiles.m[t] - M0);
+#pragma unroll
+    for (int x = 0; x < VT; ++x) tiles.acc[t][x] *= a;
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+#pragma unroll
+    for (int h = NW / 2; h >= 4; h /= 2) {
+      if (wave >= h && wave < 2 * h) {
+#pragma unroll
+        for (int x = 0; x < VT; ++x) o_s[wave - h][x][lane] = tiles.acc[t][x];
+      }
+      __syncthreads();
+      if (wave < h) {
+#pragma unroll
+        for (int x = 0; x < VT; ++x) tiles.acc[t][x] += o_s[wave][x][lane];
+      }
+      __syncthreads();
+    }
+    if (wave < 4) {
+#pragma unroll
+      for (int x = 0; x < VT; ++x) o_s[wave][x][lane] = tiles.acc[t][x];
+    }
+    __syncthreads();
+    for (int x = wave; x < VT; x += NW) {
+      const f32x4 o = (o_s[0][x][lane] + o_s[1][x][lane]) + (o_s[2][x][lane] + o_s[3][x][lane]);
+      tree_finish4(p, D, pair, b, hk, split, 16 * t + lr, R, node[t], 16 * x + 4 * lq, M[t], L[t], o);
+    }
+    if (t + 1 < MT) __syncthreads();
+  }
+}
+
+// More than 64 rows: the waves have rows of their own, 16 MT each, and walk the same items, which come through LDS, two buffers in turn: an operand is loaded once for 16 MT NW
+// rows.  What bounds it is the matrix cores (6 D products per row and 64 keys, with the pairs) and, beside them, the exponentials.
+template <int D, int MT, int NW, bool QF32, bool SPARSE>
+__global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
+  constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D, PIECES = 4 * D, PER = 2 * PIECES / (64 * NW);   // 16-byte pieces of K (and of V) in an item; of both per thread
+  static_assert(PER >= 1, "");
+  __shared__ __attribute__((aligned(16))) u32x4 kv_s[2][2 * PIECES];
+  __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
+  __shared__ int sums_s[NW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
+  const int split = blockIdx.x % p.nsplit, rb = blockIdx.x / p.nsplit, hk = blockIdx.y, b = blockIdx.z, R = p.T * p.G, r0 = (rb * NW + wave) * 16 * MT;
+  const long pair = (long)b * p.kv + hk;
+  int len, there;
+  tree_extent(p, b, len, there);
+  mask64 anc; bool ok;
+  tree_ancestors(p.parent ? p.parent + (long)b * p.T : nullptr, p.T, there, lane, anc, ok);
+  const mask64 present = __ballot(ok);
+  mask64 seen[MT]; int node[MT]; bool row_ok[MT];
+  bf16x8 qh[MT][KS], ql[QF32 ? MT : 1][KS];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int r = r0 + 16 * t + lr;
+    tree_row(p, r, R, anc, node[t], seen[t], row_ok[t]);
+    bf16x8 lo;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[t][x], lo); if constexpr (QF32) ql[t][x] = lo; }
+  }
+  const int ngr = (len + there + 31) >> 5;
+  TreeItems it{0, 0, ngr, nullptr, 1};
+  const unsigned* picks = nullptr;
+  if constexpr (SPARSE) {
+    picks = p.chosen + pair * p.T * p.words;
+    const int done = len / (32 * p.bg), w0 = rb * NW * 16 * MT, w1 = min(R, w0 + NW * 16 * MT);
+    it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
+    it.listed = tree_list(picks, p.words, w0 / p.G, (w1 + p.G - 1) / p.G, done, list_s, sums_s) * p.bg;
+    it.n = it.listed + ngr - it.tail0;
+  }
+  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
+  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + (size_t)pair * p.cap * D);
+  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + (size_t)pair * p.cap * D);
+  TreeTiles<D, MT, QF32> tiles;
+  tiles.clear();
+  u32x4 kvn[PER];                                // (a wave's pieces are all of K or all of V)
+  auto ask = [&](int g) {
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int z = (wave + x * NW) * 64;
+      kvn[x] = (z < PIECES ? Kb + (size_t)g * (GRP / 8) + z : Vb + (size_t)g * (GRP / 8) + z - PIECES)[lane];
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int x = 0; x < PER; ++x) kv_s[buf][tid + x * 64 * NW] = kvn[x];
+  };
+  int g = 0;
+  if (i0 < i1) { g = __builtin_amdgcn_readfirstlane(it.group(i0)); ask(g); put(0); }
+  __syncthreads();
+  for (int i = i0; i < i1; ++i) {
+    const int buf = (i - i0) & 1;
+    const int gn = i + 1 < i1 ? __builtin_amdgcn_readfirstlane(it.group(i + 1)) : g;
+    unsigned word[SPARSE ? MT : 1];
+    if constexpr (SPARSE) {
+      const int blk = g / p.bg;
+#pragma unroll
+      for (int t = 0; t < MT; ++t) word[t] = i < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
+    }
+    if (i + 1 < i1) ask(gn);
+    u32x4 kf[2 * KS], vf[VT];
+#pragma unroll
+    for (int x = 0; x < 2 * KS; ++x) kf[x] = kv_s[buf][x * 64 + lane];
+#pragma unroll
+    for (int x = 0; x < VT; ++x) vf[x] = kv_s[buf][PIECES + x * 64 + lane];
+    bool vis[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && word[t]; }
+    const int at = 32 * g + 8 * lq - len;
+    const bool edge = 32 * g + 32 > len;
+    if (edge) tree_blank<VT>(vf, at, present);
+    tiles.item(kf, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; }, [&](int t, int x) { return ql[QF32 ? t : 0][x]; });
+    if (i + 1 < i1) put(buf ^ 1);
+    __syncthreads();
+    g = gn;
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const float L = sum_rows(tiles.l[t]);
+#pragma unroll
+    for (int x = 0; x < VT; ++x) tree_finish4(p, D, pair, b, hk, split, r0 + 16 * t + lr, R, node[t], 16 * x + 4 * lq, tiles.m[t], L, tiles.acc[t][x]);
   }
 }
 
@@ -332,7 +515,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
-  const int split = blockIdx.x % p.nsplit, hk = blockIdx.x / p.nsplit, rb = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x % p.nsplit, rb = blockIdx.x / p.nsplit, hk = blockIdx.y, b = blockIdx.z;
   const int R = p.T * p.G, r0 = rb * 16;
   int len, there;
   tree_extent(p, b, len, there);
@@ -350,7 +533,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const long at = (long)b * p.q_seq + (long)node * p.q_row + (long)(hk * p.G + row - node * p.G) * p.q_head + 16 * x + 4 * lq + j;
-      q[x][j] = !row_ok ? 0.f : (p.q_f32 ? ((const float*)p.q)[at] : bf2f(((const bf16_t*)p.q)[at]));
+      q[x][j] = !row_ok ? 0.f : p.sign * (p.q_f32 ? ((const float*)p.q)[at] : bf2f(((const bf16_t*)p.q)[at]));
     }
   const int ngr = (len + there + 31) >> 5;
   TreeItems it{0, 0, ngr, nullptr, 1};
@@ -428,7 +611,6 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
 #pragma unroll
   for (int x = 0; x < VT; ++x) o_s[wave][x][lane] = acc[x];
   __syncthreads();
-  float* part = p.part + ((((long)b * p.kv + hk) * gridDim.y + rb) * p.nsplit + split) * 16 * (D + 2);
   for (int x = wave; x < VT; x += 4) {
     float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -441,36 +623,43 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
       L = fmaf(l_s[w][lr], a, L);
       o += o_s[w][x][lane] * a;
     }
-    if (p.nsplit > 1) {
-      *(f32x4*)(part + lr * D + 16 * x + 4 * lq) = o;
-      if (x == 0 && lq == 0) { part[16 * D + lr] = M; part[16 * (D + 1) + lr] = L; }
-    } else if (row < R) {
-      tree_store4(p, b, node, hk * p.G + row - node * p.G, 16 * x + 4 * lq, row_ok && L > 0.f ? o / L : (row_ok && L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
-    }
+    tree_finish4(p, D, (long)b * p.kv + hk, b, hk, split, row, R, node, 16 * x + 4 * lq, M, L, o);
   }
 }
 
-// Partial results of the splits joined:  out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  A row per D / 4 lanes, RB rows per row block.
-template <int D>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeP p, int RB) {
-  constexpr int Q = D / 4;                       // lanes of a row
-  const int R = p.T * p.G, blocks = (R + RB - 1) / RB;
-  const long id = (long)blockIdx.x * (256 / Q) + threadIdx.x / Q;      // (row, key head, sequence)
-  if (id >= (long)p.B * p.kv * R) return;
-  const int c = threadIdx.x % Q * 4, r = (int)(id % R), rb = r / RB, rr = r - rb * RB;
-  const long pair = id / R;
-  const int hk = (int)(pair % p.kv), b = (int)(pair / p.kv), node = r / p.G;
-  const long step = (long)RB * (D + 2);
-  const float* part = p.part + (pair * blocks + rb) * p.nsplit * step;
-  float M = -INFINITY, L = 0.f;
-  for (int s = 0; s < p.nsplit; ++s) M = fmaxf(M, part[s * step + RB * D + rr]);
+// Partial results of the splits joined:  out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  NG x D / 4 threads per row, each with every NG-th split, that meet in LDS: a
+// chain of three trips to memory whatever the number of splits.
+template <int D, int NG>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeP p) {
+  constexpr int Q = D / 4, PER = 256 / (Q * NG);
+  __shared__ __attribute__((aligned(16))) f32x4 o_s[NG > 1 ? 256 : 1];
+  __shared__ float l_s[NG > 1 ? 256 : 1];
+  const int R = p.T * p.G, tid = threadIdx.x, c = tid % Q, ng = tid / Q % NG;
+  const long id = (long)blockIdx.x * PER + tid / (Q * NG), pairs = (long)p.B * p.kv, rows = pairs * p.nsplit * R;
+  const bool live = id < pairs * R;
+  const long pair = live ? id / R : 0;
+  const int r = live ? (int)(id - pair * R) : 0;
+  const long at = pair * p.nsplit * R + r;
+  const float *ms = p.part + rows * D + at, *ls = ms + rows;
+  float M = -INFINITY;
+#pragma unroll 8
+  for (int s = 0; s < p.nsplit; ++s) M = fmaxf(M, ms[(long)s * R]);
   const float M0 = M == -INFINITY ? 0.f : M;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < p.nsplit; ++s) {
-    const float a = exp2f(part[s * step + RB * D + rr] - M0);
-    L = fmaf(part[s * step + RB * (D + 1) + rr], a, L);
-    o += *(const f32x4*)(part + s * step + rr * D + c) * a;
+  float L = 0.f;
+#pragma unroll 4
+  for (int s = ng; s < p.nsplit; s += NG) {
+    const float a = exp2f(ms[(long)s * R] - M0);
+    L = fmaf(ls[(long)s * R], a, L);
+    o += *(const f32x4*)(p.part + (at + (long)s * R) * D + 4 * c) * a;
   }
-  // (an absent node has seen nothing anywhere: L = 0)
-  tree_store4(p, b, node, hk * p.G + r - node * p.G, c, L > 0.f ? o / L : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
+  if constexpr (NG > 1) {
+    o_s[tid] = o; l_s[tid] = L;
+    __syncthreads();
+    if (ng) return;
+    for (int n = 1; n < NG; ++n) { o += o_s[tid + n * Q]; L += l_s[tid + n * Q]; }
+  }
+  if (!live) return;
+  const int node = r / p.G, hk = (int)(pair % p.kv), b = (int)(pair / p.kv);
+  tree_store4(p, b, node, hk * p.G + r - node * p.G, 4 * c, L > 0.f ? o / L : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
 }

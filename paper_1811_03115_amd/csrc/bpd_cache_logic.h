@@ -36,21 +36,25 @@ inline size_t summaries_elements(const bpd_cache& c, int block) {
   return (size_t)c.max_batch * c.n_kv_heads * tiles * 2 * c.head_dim * 64;
 }
 
-struct TreePlan { int mt, blocks, nsplit; size_t chosen_at, score_at, bytes; };
-// Row tiles of 16 per workgroup, row blocks, parts that the keys are split into, and what the workspace holds: partial results, then (block > 0) bits of the chosen blocks
-// and their bounds.
+struct TreePlan { bool rows; int mt, waves, blocks, nsplit; size_t chosen_at, score_at, bytes; };
+// Kernel (rows: the waves share the keys), row tiles of 16 and waves per workgroup, row blocks, parts that the keys are split into, and what the workspace holds: partial
+// results, then (block > 0) bits of the chosen blocks and their bounds.
 inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int block, int cus) {
   TreePlan p{};
   const int R = T * (heads / c.n_kv_heads);
-  p.mt = !cache_grouped(c) || R <= 16 ? 1 : (R <= 32 || c.head_dim == 128 ? 2 : 4);
-  p.blocks = (R + 16 * p.mt - 1) / (16 * p.mt);
+  const bool grouped = cache_grouped(c);
+  p.rows = grouped && R > 64;
+  if (p.rows) { p.mt = 2; p.waves = R > 128 ? 8 : 4; }
+  else { p.mt = grouped ? (R + 15) / 16 : 1; p.waves = 4; }
+  const int per = p.rows ? 16 * p.mt * p.waves : (grouped ? 64 : 16);
+  p.blocks = (R + per - 1) / per;
   const long pairs = (long)B * c.n_kv_heads * p.blocks, groups = (c.capacity + 31) / 32;
   long n = (2L * cus + pairs - 1) / pairs, most = groups / 8;
   n = n < most ? n : most;
   n = n < 64 ? n : 64;
   p.nsplit = n < 1 ? 1 : (int)n;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  p.bytes = p.nsplit > 1 ? up((size_t)pairs * p.nsplit * (16 * p.mt) * (c.head_dim + 2) * 4) : 0;
+  p.bytes = p.nsplit > 1 ? up((size_t)B * c.n_kv_heads * p.nsplit * R * (c.head_dim + 2) * 4) : 0;
   if (block && c.capacity / block > 0) {
     const size_t nb = c.capacity / block, rows = (size_t)B * c.n_kv_heads * T;
     p.chosen_at = p.bytes; p.bytes += up(rows * ((nb + 31) / 32) * 4);
