@@ -36,7 +36,7 @@
  * Pointer arguments marked [host|device] may be either; arguments marked [device] are
  * dereferenced by kernels.
  *
- * Capture.  bpd_encode, bpd_step, bpd_step_static, bpd_set_proposals and bpd_debug_step_logits can
+ * Capture.  bpd_encode, bpd_step, bpd_step_tree, bpd_step_static, bpd_set_proposals and bpd_debug_step_logits can
  * be captured into a HIP graph on the context's stream and replayed any number of times, with
  * direct calls in between (the calls that wait cannot).  Settings (bpd_set_*), B, S and k are
  * those of the capture; arrays are read and written where they were: device arrays by the kernels,
@@ -186,6 +186,20 @@ int bpd_encode(bpd_ctx* ctx, const int32_t* src_ids, const int32_t* src_len,
  * Errors: BPD_E_STATE (no bpd_encode yet), BPD_E_ARG. */
 int bpd_step(bpd_ctx* ctx, int k, const int32_t* imposed_accept, int32_t* accepted_len);
 
+/* One step whose k rows are the nodes of a tree instead of a chain (all sequences have the same tree): the first node
+ * is P_1, every other one continues the node `parent` names, at that node's position plus one, and sees the prefix, its
+ * ancestors and itself.  Verified exactly, along the branches: P_1 is taken, then the first child of the last taken node whose
+ * token is p_1's arg-max there, and so on; the tokens are greedy decoding's whatever the tree holds.  Cut as in bpd_step (EOS, max_len).
+ *   parent [host] int32 [k]: -1, then 0 .. i - 1 for node i.  The proposals P (bpd_get_state, bpd_set_proposals) are the nodes' tokens.
+ *   accepted_len as in bpd_step.
+ * The next proposals are made for the same tree: node i, e nodes below the first one and r-th child of its parent, is given what head
+ * e + r + 1 says at the r-th taken node before the last, or (no such head or node) head e + 1 at the last.  For a chain that is
+ * bpd_step's row k-hat.  (bpd_encode and bpd_step leave head i + 1's token in node i, whatever its depth: a tree whose first nodes
+ * are a chain has that right from the start.)
+ * Two-phase scoring does not apply; rows of sequences that have ended are computed and ignored; the layers run kernel by kernel.
+ * Errors: BPD_E_STATE, BPD_E_ARG (also with relaxed verification or local attention set). */
+int bpd_step_tree(bpd_ctx* ctx, int k, const int32_t* parent, int32_t* accepted_len);
+
 /* bpd_step for callers that cannot allocate device memory and cannot spare workspace for a step's scratch: code
  * under HIP graph capture, tight serving loops, harnesses that forbid hipMalloc.  Same arguments, same results (the
  * same kernels in the same order) and the same state transition as bpd_step; the scratch of the step (arg-max keys
@@ -235,6 +249,18 @@ int bpd_set_two_phase(bpd_ctx* ctx, int on);
  * later bpd_encode / bpd_step / bpd_decode / bpd_debug_step_logits calls.  Encoder and
  * cross-attention are not affected.  Errors: BPD_E_ARG (null ctx, negative lengths). */
 int bpd_set_local_attention(bpd_ctx* ctx, int query_block, int memory_len);
+
+/* Decoder self-attention by chosen blocks (bpd_sparse_attention below): every row of a step sees, of the committed prefix, the first
+ * `first` and the last `recent` complete blocks of `block` rows (32, 64 or 128), the `top` others with the largest bound of its
+ * scores per head, and what is behind the last complete block; and the step's own rows as ever.  For long outputs, whose caches are most of
+ * what a step reads.  block = 0 (the rest is ignored) restores attention to all keys, the default; the setting may change
+ * between steps, and applies to later bpd_step / bpd_step_tree / bpd_decode / bpd_debug_step_logits calls (whose layers then run kernel by
+ * kernel).
+ *   buffer [device] caller-owned, 256-byte aligned, bpd_sparse_buffer_bytes(ctx, block), not shared with another context; it must stay
+ *       valid as long as the setting does.  Summaries of what is committed already are made here (enqueued).
+ * Errors: BPD_E_ARG (also with local attention set), BPD_E_CAPACITY (buffer; more than BPD_BLOCKS_MAX blocks). */
+int bpd_set_sparse_attention(bpd_ctx* ctx, int block, int first, int recent, int top, void* buffer, size_t bytes);
+size_t bpd_sparse_buffer_bytes(const bpd_ctx* ctx, int block);   /* 0: no such block */
 
 /* The decoding loop of Section 3 with the merged verify / predict invocation of Section 4:
  * repeat bpd_step until every sequence has ended or max_steps steps were made; waits for the end

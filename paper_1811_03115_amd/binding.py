@@ -59,6 +59,7 @@ EXPORTS = ["bpd_workspace_bytes", "bpd_create", "bpd_destroy", "bpd_load_weights
            "bpd_set_acceptance", "bpd_set_top_n", "bpd_set_two_phase", "bpd_set_local_attention", "bpd_decode", "bpd_get_state", "bpd_get_output", "bpd_get_stats",
            "bpd_set_proposals", "bpd_debug_step_logits", "bpd_profile_enable", "bpd_profile_read",
            "bpd_profile_samples", "bpd_measure_hbm_read", "bpd_measure_mfma_bf16", "bpd_last_error",
+           "bpd_step_tree", "bpd_set_sparse_attention", "bpd_sparse_buffer_bytes",
            "bpd_op_error", "bpd_cache_bytes", "bpd_summaries_bytes", "bpd_attention_workspace_bytes", "bpd_cache_store", "bpd_tree_attention",
            "bpd_sparse_attention", "bpd_tree_accept"]
 
@@ -98,6 +99,10 @@ def lib() -> C.CDLL:
         L.bpd_profile_samples.argtypes = [vp, vp, C.c_int64, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.bpd_measure_hbm_read.argtypes = [vp, C.c_size_t, vp, C.c_int, C.POINTER(C.c_double)]
         L.bpd_measure_mfma_bf16.argtypes = [vp, vp, C.c_int, C.POINTER(C.c_double)]
+        L.bpd_step_tree.argtypes = [vp, C.c_int, i32p, i32p]
+        L.bpd_set_sparse_attention.argtypes = [vp] + [C.c_int] * 4 + [vp, C.c_size_t]
+        L.bpd_sparse_buffer_bytes.restype = C.c_size_t
+        L.bpd_sparse_buffer_bytes.argtypes = [vp, C.c_int]
         cp, rp, sz = C.POINTER(bpd_cache), C.POINTER(bpd_rows), C.c_size_t
         L.bpd_op_error.restype = C.c_char_p
         L.bpd_op_error.argtypes = []
@@ -362,6 +367,25 @@ class Context:
     def bpd_step_static(self, k: int, imposed_accept=None, accepted_len=None):
         imposed_accept = _i32(imposed_accept)
         self._check(self.L.bpd_step_static(self.h, k, _ptr(imposed_accept), _ptr(accepted_len)))
+
+    def bpd_step_tree(self, k: int, parent, accepted_len=None):
+        """parent: k ints on the host (list, tuple or numpy): -1, then an earlier node for each."""
+        parent = np.ascontiguousarray(parent, dtype=np.int32)
+        if parent.shape != (k,):
+            raise BpdError(-1, "parent: one of each node")
+        self._check(self.L.bpd_step_tree(self.h, k, _ptr(parent), _ptr(accepted_len)))
+
+    def bpd_sparse_buffer_bytes(self, block: int) -> int:
+        return self.L.bpd_sparse_buffer_bytes(self.h, block)
+
+    def bpd_set_sparse_attention(self, block: int, first: int = 1, recent: int = 2, top: int = 8):
+        """block 0: all keys again.  The context keeps the buffer."""
+        torch = self.torch
+        nbytes = self.bpd_sparse_buffer_bytes(block) if block else 0
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device) if nbytes else None
+        self._check(self.L.bpd_set_sparse_attention(self.h, block, first, recent, top, (buf.data_ptr() + 255) // 256 * 256 if buf is not None else None, nbytes))
+        self.sparse_buffer = buf
 
     def bpd_set_acceptance(self, distance_eps: int = 0, min_block: int = 1):
         self._check(self.L.bpd_set_acceptance(self.h, distance_eps, min_block))

@@ -5,6 +5,8 @@
 #include "bpd_kernels.h"
 #include "bpd_stack.h"
 #include "bpd_host_logic.h"
+#include "bpd_cache_launch.h"
+#include "bpd_cache_logic.h"
 
 #include <cmath>
 #include <cstdio>
@@ -52,6 +54,9 @@ struct bpd_ctx {
   int64_t steps = 0;              // steps enqueued since bpd_encode: bounds the cache lengths (the count itself is on the device, StateP::steps_done)
   int distance_eps = 0, min_block = 1, top_n = 1, two_phase = 0;
   int local_q = 0, local_m = 0;   // 1D local self-attention in the decoder (0: full causal), bpd_set_local_attention
+  unsigned long long tree = 0;         // the tree of the step being run (tree_parent(); 0: a chain), bpd_step_tree
+  bpd_blocks sparse{};                 // self-attention by chosen blocks (block 0: of all keys), bpd_set_sparse_attention: summaries of all layers, scratch behind them
+  char* sparse_scratch = nullptr; size_t sparse_scratch_bytes = 0;
   int num_cus = 256;                   // compute units of the device the context was created on
   int device = 0;                      // that device's index
   // decoder stack kernel: placement of workgroups on XCDs as probed at creation (workers = 0: not usable), the value
@@ -717,15 +722,15 @@ void embed(bpd_ctx* ctx, const int* tok, int tok_ld, const int* base, int rows_p
   const float scale = sqrtf((float)c.d_model);
   if (stats_path(ctx, M) && x == ctx->lay.x) {
     hipLaunchKernelGGL(embed_stats_kernel, dim3(c.d_model / 16), dim3(64), 0, ctx->stream, tok, tok_ld, base, rows_per_seq, M,
-                       c.d_model, (const bf16_t*)ctx->lay.emb, c.vocab, pos, scale, x, zero_input, ctx->lay.stats_ln, keys, nkeys, seq);
+                       c.d_model, (const bf16_t*)ctx->lay.emb, c.vocab, pos, scale, x, zero_input, ctx->lay.stats_ln, keys, nkeys, seq, ctx->tree);
     return;
   }
   if (c.dtype == BPD_BF16)
     hipLaunchKernelGGL(embed_kernel<true>, grid, dim3(256), 0, ctx->stream, tok, tok_ld, base, rows_per_seq, M, c.d_model,
-                       ctx->lay.emb, c.vocab, pos, scale, x, zero_input, keys, nkeys, seq);
+                       ctx->lay.emb, c.vocab, pos, scale, x, zero_input, keys, nkeys, seq, ctx->tree);
   else
     hipLaunchKernelGGL(embed_kernel<false>, grid, dim3(256), 0, ctx->stream, tok, tok_ld, base, rows_per_seq, M, c.d_model,
-                       ctx->lay.emb, c.vocab, pos, scale, x, zero_input, keys, nkeys, seq);
+                       ctx->lay.emb, c.vocab, pos, scale, x, zero_input, keys, nkeys, seq, ctx->tree);
 }
 
 void fill_i32(bpd_ctx* ctx, int* p, long n, int v) {
@@ -1043,6 +1048,29 @@ void lean_ffn(bpd_ctx* ctx, float* x, LnW ln, void* xn, const void* w1, const fl
   lean_residual(ctx, hidden, F, w2, b2, M, x);
 }
 
+// The decoder's self-attention caches as the cache operators take them: all layers, or layer l
+bpd_cache self_cache(const bpd_ctx* ctx, int l = -1) {
+  const bpd_config& c = ctx->cfg;
+  const size_t rows = kv_rows(c, (size_t)c.max_out_len + c.k_max + 1), layer = (size_t)c.max_batch * rows * c.d_model * act_size(c);
+  const size_t at = l < 0 ? 0 : layer * l;
+  return bpd_cache{(char*)ctx->lay.selfK + at, (char*)ctx->lay.selfV + at, c.dtype, l < 0 ? c.n_dec_layers : 1, c.max_batch, c.n_heads, c.d_model / c.n_heads, (int32_t)rows};
+}
+// Self-attention of R rows per sequence, whose keys and values are in layer l's cache: of a chain over all of it, or of a tree, or over chosen blocks
+void self_attention(bpd_ctx* ctx, int l, const void* Kl, const void* Vl, int slots, int B, int R, const int* base, const int* seq, bool packed) {
+  const Layout& L = ctx->lay;
+  if (!ctx->tree && !ctx->sparse.block) { attention(ctx, L.q, Kl, Vl, L.attn, slots, B, R, base, 1, seq, packed); return; }
+  const int dh = ctx->cfg.d_model / ctx->cfg.n_heads;
+  BlockAttention a{self_cache(ctx, l), L.q, L.attn, packed, base, seq, ctx->tree, B, R, ctx->cfg.n_heads, 1.0f / sqrtf((float)dh), nullptr, 0,
+                   L.attn_part, (size_t)ATTN_PART_SLOTS * 16 * (dh + 2) * 4, ctx->num_cus};
+  bpd_blocks blocks = ctx->sparse;
+  if (blocks.block) {
+    blocks.summaries = (char*)blocks.summaries + (size_t)l * summaries_elements(a.cache, blocks.block) * cache_element(a.cache);
+    a.blocks = &blocks; a.added = ctx->cfg.k_max;         // (no step commits more, and each summarises what the one before has left)
+    a.scratch = ctx->sparse_scratch; a.scratch_bytes = ctx->sparse_scratch_bytes;
+  }
+  launch_block_attention(a, ctx->stream);
+}
+
 // One invocation of the combined model on R new rows per sequence (R = 1 for the first call
 // on the empty prefix, R = k afterwards) with the first k heads; fills keys[B*R*k].
 int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
@@ -1075,12 +1103,13 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
     PhaseTimer t(ctx, BPD_PHASE_LAYERS);
     // (the previous step's accept kernel may already have embedded this block, with its statistics (and, beyond 16 rows,
     // its bf16 copy in L.xn), and cleared the keys)
-    const bool have_x = embed_in_accept(ctx) && !zero_input && R == k && ctx->x_ready_k == k && ctx->x_ready_slots == B && !(logits && slots_used(ctx));
+    const bool have_x = embed_in_accept(ctx) && !ctx->tree && !zero_input && R == k && ctx->x_ready_k == k && ctx->x_ready_slots == B && !(logits && slots_used(ctx));
     ctx->x_ready_k = 0;
     xs = have_x && !sp;
     if (!have_x) embed(ctx, L.P, c.k_max, base, R, M, L.pos_tgt, L.x, zero_input, L.keys, (int)nk, seq);
-    const bool stack = M <= 16 && (lean || sp) && stack_usable(ctx, B, R);
-    const int way = stack || !lean ? LAYERS_CHAIN : layers_way(ctx, B, R);
+    const bool own_keys = !ctx->tree && !ctx->sparse.block;       // (the kernels of all layers attend to all keys of a chain)
+    const bool stack = own_keys && M <= 16 && (lean || sp) && stack_usable(ctx, B, R);
+    const int way = stack || !lean || !own_keys ? LAYERS_CHAIN : layers_way(ctx, B, R);
     const bool one = way != LAYERS_CHAIN;
     if (stack) launch_stack(ctx, R);
     else if (one) launch_layers(ctx, R, way);
@@ -1099,7 +1128,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
           lean_ln_gemm<RG_QKV>(ctx, L.x, w.ln1, L.xn, q);
         } else {
           lean_ln_gemm<RG_QKV>(ctx, L.x, w.ln1, L.xn, rg_kv(ctx, nullptr, w.wqkv, M, 3 * d, kv));
-          attention(ctx, L.q, Kl, Vl, L.attn, slots, B, R, base, 1, seq, lean);
+          self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean);
         }
         lean_residual(ctx, L.attn, d, w.wo, nullptr, M, L.x);
         if (qproj) {
@@ -1115,7 +1144,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
       }
       // self-attention sublayer: K/V of the block rows go straight into the cache at L_b + i'
       gemm_ln(ctx, L.x, w.ln1, L.xn, nullptr, gp(L.xn, d, w.wqkv, 3 * d, M, 3 * d, d), kv, sp, xs, folds ? &w.f_qkv : nullptr);
-      attention(ctx, L.q, Kl, Vl, L.attn, slots, B, R, base, 1, seq, lean);
+      self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean);
       xs = gemm(ctx, gp(L.attn, d, w.wo, d, M, d, d), residual(nullptr, d));
       // cross-attention sublayer over the encoder memory
       if (qproj) {
@@ -1132,7 +1161,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
     }
   }
   { PhaseTimer t(ctx, BPD_PHASE_EMPTY); }       // calibration of the event bracketing itself
-  if (ctx->two_phase && R == k && k > 1 && M > 16 && !logits && c.dtype == BPD_BF16) return heads_two_phase(ctx, k);
+  if (ctx->two_phase && !ctx->tree && R == k && k > 1 && M > 16 && !logits && c.dtype == BPD_BF16) return heads_two_phase(ctx, k);
   // the k residual FFN heads: final LayerNorm + hidden layers side by side (h kept in fp32
   // for the residual), then one output layer per head
   {
@@ -1168,7 +1197,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
     PhaseTimer t(ctx, BPD_PHASE_VOCAB);
     // top-n acceptance: the scores of head 1 (every k-th row of O) are kept, for the rank of each proposal among them (a second pass
     // over the vocabulary for those rows alone, as before, was 13 us of a step of 13 slots, k = 6, over 32 000 tokens at d = 512)
-    const bool rank = ctx->top_n > 1 && R == k && k > 1;
+    const bool rank = ctx->top_n > 1 && !ctx->tree && R == k && k > 1;
     float* const kept = logits ? logits : (rank ? L.logits_h1 : nullptr);
     const int lstep = logits ? 1 : k;
     if (c.dtype == BPD_BF16) {
@@ -1209,7 +1238,7 @@ SmallLds small_decode_lds(const bpd_config& c, int rows, int k, int hgroup, bool
 // there may be and `more` others are faster launch by launch (about the mean of those lengths)
 int small_hgroup(const bpd_ctx* ctx, int k, long more) {
   const bpd_config& c = ctx->cfg;
-  if (!small_shape(c)) return 0;
+  if (!small_shape(c) || ctx->sparse.block) return 0;
   const long cap = c.max_out_len + c.k_max + 1, from = std::min(cap, (long)ctx->steps * c.k_max + 1 + k);
   long keys = (from + std::min(cap, from + more)) / 2;
   if (ctx->local_q > 0) keys = std::min(keys, (long)ctx->local_q + ctx->local_m + k);
@@ -1848,6 +1877,40 @@ int bpd_step(bpd_ctx* ctx, int k, const int32_t* imposed_accept, int32_t* accept
   return BPD_OK;
 }
 
+int bpd_step_tree(bpd_ctx* ctx, int k, const int32_t* parent, int32_t* accepted_len) {
+  if (!ctx) return BPD_E_ARG;
+  if (!ctx->encoded) return fail(ctx, BPD_E_STATE, "bpd_step_tree: call bpd_encode first");
+  if (k < 1 || k > ctx->cfg.k_max || !parent) return fail(ctx, BPD_E_ARG, "bpd_step_tree: k outside 1..k_max, or null parent");
+  if (ctx->distance_eps || ctx->min_block > 1 || ctx->top_n > 1 || ctx->local_q) return fail(ctx, BPD_E_ARG, "bpd_step_tree: trees are verified exactly, with full attention (or by chosen blocks)");
+  unsigned long long tree = 15;
+  if (parent[0] != -1) return fail(ctx, BPD_E_ARG, "bpd_step_tree: the first node's parent is -1");
+  for (int i = 1; i < k; ++i) {
+    if (parent[i] < 0 || parent[i] >= i) return fail(ctx, BPD_E_ARG, "bpd_step_tree: a node's parent is an earlier node");
+    tree |= (unsigned long long)parent[i] << (4 * i);
+  }
+  Layout& L = ctx->lay;
+  forget_replayed(ctx);
+  const bool out_host = accepted_len && is_host_ptr(accepted_len);
+  std::fill(ctx->remaining.begin(), ctx->remaining.end(), -1);
+  ctx->live1 = ctx->live2 = -1;
+  {
+    PhaseTimer whole(ctx, BPD_PHASE_STEP);
+    use_slots(ctx, ctx->B);                      // rows of every sequence, ended or not
+    ctx->tree = tree;
+    const int rc = step_forward(ctx, k, nullptr, 0, 0);
+    ctx->tree = 0;
+    if (rc) return rc;
+    PhaseTimer t(ctx, BPD_PHASE_ACCEPT);
+    int* path = L.topn_ok;                       // (not in use: top_n is 1)
+    hipLaunchKernelGGL(accept_tree_kernel, dim3(ctx->B), dim3(64), 0, ctx->stream, state_params(ctx), L.keys, k, ctx->B, tree, out_host ? nullptr : accepted_len, path, slots_used(ctx));
+    launch_tree_move(self_cache(ctx), path, ctx->cfg.k_max, L.accepted, L.L, ctx->B, ctx->stream);
+  }
+  LAUNCHCHK();
+  ctx->steps++;
+  if (out_host) HIPCHK(hipMemcpyAsync(accepted_len, L.accepted, (size_t)ctx->B * 4, hipMemcpyDeviceToHost, ctx->stream));
+  return BPD_OK;
+}
+
 int bpd_step_static(bpd_ctx* ctx, int k, const int32_t* imposed_accept, int32_t* accepted_len) {
   if (!ctx) return BPD_E_ARG;
   if (!ctx->encoded) return fail(ctx, BPD_E_STATE, "bpd_step_static: call bpd_encode first");
@@ -1868,7 +1931,7 @@ int bpd_step_static(bpd_ctx* ctx, int k, const int32_t* imposed_accept, int32_t*
     const size_t wgs = (size_t)c.n_heads * ctx->B * ((k + 15) / 16);
     if (ns > 1) attn_b = std::max(attn_b, up(ns * wgs * 16 * (d / c.n_heads + 2) * 4));
   }
-  if (layers_way(ctx, ctx->B, k) == LAYERS_JOBS && layers_split_of(ctx, ctx->B, k) > 1) attn_b = std::max(attn_b, up((size_t)layers_split_of(ctx, ctx->B, k) * c.n_heads * ctx->B * 16 * 66 * 4));
+  if (!ctx->sparse.block && layers_way(ctx, ctx->B, k) == LAYERS_JOBS && layers_split_of(ctx, ctx->B, k) > 1) attn_b = std::max(attn_b, up((size_t)layers_split_of(ctx, ctx->B, k) * c.n_heads * ctx->B * 16 * 66 * 4));
   size_t slices = 1;
   if (lean_ok(c, (int)M)) slices = lean_slices(ctx, (int)M);
   else if (c.dtype == BPD_BF16 && M > 16)
@@ -1934,7 +1997,45 @@ int bpd_set_local_attention(bpd_ctx* ctx, int query_block, int memory_len) {
   if (!ctx) return BPD_E_ARG;
   if (query_block < 0 || memory_len < 0 || (query_block == 0 && memory_len != 0))
     return fail(ctx, BPD_E_ARG, "local attention: query_block >= 0, memory_len >= 0 (and 0 when query_block is 0)");
+  if (query_block && ctx->sparse.block) return fail(ctx, BPD_E_ARG, "local attention: not with attention by chosen blocks");
   ctx->local_q = query_block; ctx->local_m = memory_len;
+  return BPD_OK;
+}
+
+// Summaries of all layers, then the largest scratch that steps of up to max_batch sequences need
+static size_t sparse_bytes(const bpd_config& c, int block, int cus, size_t& summaries, size_t& scratch) {
+  const bpd_cache cache{nullptr, nullptr, c.dtype, c.n_dec_layers, c.max_batch, c.n_heads, c.d_model / c.n_heads, (int32_t)kv_rows(c, (size_t)c.max_out_len + c.k_max + 1)};
+  summaries = (summaries_elements(cache, block) * cache_element(cache) * c.n_dec_layers + ALIGN - 1) / ALIGN * ALIGN;
+  scratch = 0;
+  for (int T = 1; T <= c.k_max; ++T)
+    for (int B = 1; B <= c.max_batch; ++B) scratch = std::max(scratch, plan_attention(cache, B, T, c.n_heads, block, cus).bytes);
+  return summaries + scratch;
+}
+
+size_t bpd_sparse_buffer_bytes(const bpd_ctx* ctx, int block) {
+  if (!ctx || (block != 32 && block != 64 && block != 128)) return 0;
+  size_t summaries, scratch;
+  return sparse_bytes(ctx->cfg, block, ctx->num_cus, summaries, scratch);
+}
+
+int bpd_set_sparse_attention(bpd_ctx* ctx, int block, int first, int recent, int top, void* buffer, size_t bytes) {
+  if (!ctx) return BPD_E_ARG;
+  if (block == 0) { ctx->sparse = bpd_blocks{}; return BPD_OK; }
+  const bpd_config& c = ctx->cfg;
+  if ((block != 32 && block != 64 && block != 128) || first < 0 || recent < 0 || top < 0) return fail(ctx, BPD_E_ARG, "sparse attention: blocks of 32, 64 or 128 rows; first, recent and top are not negative");
+  if (ctx->local_q) return fail(ctx, BPD_E_ARG, "sparse attention: not with local attention");
+  if ((c.max_out_len + c.k_max + 1 + 31) / block > BPD_BLOCKS_MAX) return fail(ctx, BPD_E_CAPACITY, "sparse attention: more than BPD_BLOCKS_MAX blocks");
+  size_t summaries, scratch;
+  const size_t need = sparse_bytes(c, block, ctx->num_cus, summaries, scratch);
+  if (!buffer || ((uintptr_t)buffer & 255) || bytes < need) return fail(ctx, BPD_E_CAPACITY, "sparse attention: buffer null, not aligned to 256 bytes, or of less than bpd_sparse_buffer_bytes()");
+  ctx->sparse = bpd_blocks{block, first, recent, top, buffer, nullptr, nullptr};
+  ctx->sparse_scratch = (char*)buffer + summaries; ctx->sparse_scratch_bytes = scratch;
+  if (ctx->encoded)                              // what has been committed already
+    for (int l = 0; l < c.n_dec_layers; ++l) {
+      const bpd_cache cache = self_cache(ctx, l);
+      launch_summaries(cache, ctx->lay.L, ctx->B, block, (char*)buffer + (size_t)l * summaries_elements(cache, block) * cache_element(cache), ctx->stream);
+    }
+  LAUNCHCHK();
   return BPD_OK;
 }
 
@@ -2063,7 +2164,7 @@ int bpd_decode(bpd_ctx* ctx, int k, const int32_t* schedule, int max_steps, int3
     }
     // A step like the one before, of all sequences and for all of them (one sentence; images before the first ends): recorded once, replayed
     // from then on.  All sequences go on after step s - 1 for certain: there is one, or only budgets end them and none is that short.
-    bool planned = s > 0 && !ctx->two_phase && embed_in_accept(ctx) && ctx->x_ready_k == k && ctx->x_ready_slots == B && (B == 1 || (ctx->cfg.eos_id < 0 && ctx->live2 == B));
+    bool planned = s > 0 && !ctx->two_phase && !ctx->sparse.block && embed_in_accept(ctx) && ctx->x_ready_k == k && ctx->x_ready_slots == B && (B == 1 || (ctx->cfg.eos_id < 0 && ctx->live2 == B));
     for (int b = 0; planned && B > 1 && b < B; ++b) planned = rem[b] > (know ? 0 : k);
     if (planned) {
       use_slots(ctx, B);

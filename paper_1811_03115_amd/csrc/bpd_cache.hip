@@ -2,6 +2,7 @@
 // their arguments, and they run on the current device and the stream that they are given.
 #include "../../include/bpd.h"
 #include "bpd_cache_ops.h"
+#include "bpd_cache_launch.h"
 #include "bpd_cache_logic.h"
 
 #include <atomic>
@@ -94,6 +95,31 @@ void attend(const bpd_cache& c, const TreeP& p, const TreePlan& plan, hipStream_
   if (p.nsplit > 1) { if (D == 16) join<16>(p, s); else if (D == 64) join<64>(p, s); else join<128>(p, s); }
 }
 
+// Bounds of the blocks, with fresh summaries (no nodes: those alone), and the blocks that each node sees
+void choose_blocks(const bpd_cache& c, const BoundP& bp, hipStream_t s) {
+  const dim3 grid(bp.tiles, bp.t.kv, bp.t.B);
+  const int D = c.head_dim;
+  if (cache_grouped(c)) {
+    if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, bp);
+    else hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 128, true>), grid, dim3(256), 0, s, bp);
+  } else if (c.dtype == BPD_BF16) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 16, false>), grid, dim3(256), 0, s, bp);
+  else if (D == 16) hipLaunchKernelGGL((block_bounds_kernel<float, 16, false>), grid, dim3(256), 0, s, bp);
+  else if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<float, 64, false>), grid, dim3(256), 0, s, bp);
+  else hipLaunchKernelGGL((block_bounds_kernel<float, 128, false>), grid, dim3(256), 0, s, bp);
+  if (bp.t.T > 0) hipLaunchKernelGGL(block_pick_kernel, dim3(bp.t.T, bp.t.kv, bp.t.B), dim3(PICK_T), 0, s, bp);
+}
+// What the blocks of a call are, and where their bounds and bits go
+BoundP bound_args(TreeP& p, const bpd_cache& c, const bpd_blocks& blocks, unsigned* chosen, double* score) {
+  BoundP bp{};
+  const int nb = c.capacity / blocks.block;
+  p.words = (nb + 31) / 32; p.bg = blocks.block / 32; p.chosen = chosen;
+  bp.t = p;
+  bp.summaries = blocks.summaries; bp.tiles = (nb + 63) / 64;
+  bp.block = blocks.block; bp.first = blocks.first; bp.recent = blocks.recent; bp.top = blocks.top;
+  bp.added = blocks.added; bp.added_all = -1; bp.score = score; bp.chosen = chosen;
+  return bp;
+}
+
 // What bpd_tree_attention and bpd_sparse_attention check alike; null: nothing is wrong
 const char* attention_wrong(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, int B, int T, int heads, float scale) {
   if (const char* w = cache_wrong(c)) return w;
@@ -121,6 +147,39 @@ TreeP attention_args(const bpd_cache& c, const bpd_rows& q, const bpd_rows& out,
 }
 
 }  // namespace
+
+void launch_block_attention(const BlockAttention& a, hipStream_t stream) {
+  const bpd_cache& c = a.cache;
+  const int dh = c.head_dim, d = a.heads * dh, block = a.blocks ? a.blocks->block : 0;
+  const bpd_rows q{a.q, BPD_F32, 0, (int64_t)a.T * d, d, dh}, out{a.out, c.dtype, 0, (int64_t)a.T * d, d, dh};
+  TreeP p = attention_args(c, q, out, a.length, nullptr, a.B, a.T, a.heads, a.scale);
+  p.seq = a.seq; p.tree = a.tree; p.packed = a.packed ? d : 0;
+  TreePlan plan = plan_attention(c, a.B, a.T, a.heads, block, a.cus);
+  p.part = (float*)a.scratch;
+  const size_t one = (size_t)a.B * c.n_kv_heads * a.T * (dh + 2) * 4;           // bytes of one part of the keys
+  if (!block && plan.nsplit > 1 && plan.nsplit * one > a.scratch_bytes) plan.nsplit = (int)(a.scratch_bytes / one) > 1 ? (int)(a.scratch_bytes / one) : 1;
+  p.nsplit = plan.nsplit;
+  if (!block || c.capacity < block) { attend<false>(c, p, plan, stream); return; }
+  BoundP bp = bound_args(p, c, *a.blocks, (unsigned*)((char*)a.scratch + plan.chosen_at), (double*)((char*)a.scratch + plan.score_at));
+  bp.added_all = a.added;
+  choose_blocks(c, bp, stream);
+  attend<true>(c, p, plan, stream);
+}
+void launch_summaries(const bpd_cache& c, const int* length, int B, int block, void* summaries, hipStream_t stream) {
+  if (c.capacity < block) return;
+  const bpd_rows none{};
+  TreeP p = attention_args(c, none, none, length, nullptr, B, 0, c.n_kv_heads, 1.f);
+  const bpd_blocks blocks{block, 0, 0, 0, summaries, nullptr, nullptr};
+  choose_blocks(c, bound_args(p, c, blocks, nullptr, nullptr), stream);
+}
+void launch_tree_move(const bpd_cache& c, const int* path, int ld, const int* accepted, const int* length, int B, hipStream_t s) {
+  const MoveP p{path, accepted, length, ld, c.k, c.v, (long)cache_layer_elements(c), c.n_kv_heads, c.capacity};
+  const dim3 grid(c.n_kv_heads, c.n_layers, B);
+  // (the decoder's heads have 64 dimensions, or 16)
+  if (cache_grouped(c)) hipLaunchKernelGGL((tree_move_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, p);
+  else if (c.dtype == BPD_BF16) hipLaunchKernelGGL((tree_move_kernel<bf16_t, 16, false>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tree_move_kernel<float, 16, false>), grid, dim3(256), 0, s, p);
+}
 
 extern "C" {
 
@@ -196,24 +255,8 @@ int bpd_sparse_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* 
     attend<false>(*c, p, plan, s);
     return launched("bpd_sparse_attention");
   }
-  BoundP bp{};
-  p.words = (nb + 31) / 32; p.bg = blocks->block / 32;
   unsigned* chosen = blocks->chosen ? blocks->chosen : (unsigned*)((char*)workspace + plan.chosen_at);
-  p.chosen = chosen;
-  bp.t = p;
-  bp.summaries = blocks->summaries; bp.tiles = (nb + 63) / 64;
-  bp.block = blocks->block; bp.first = blocks->first; bp.recent = blocks->recent; bp.top = blocks->top;
-  bp.added = blocks->added; bp.score = (double*)((char*)workspace + plan.score_at); bp.chosen = chosen;
-  const dim3 grid(bp.tiles, p.kv, B);
-  const int D = c->head_dim;
-  if (cache_grouped(*c)) {
-    if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, bp);
-    else hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 128, true>), grid, dim3(256), 0, s, bp);
-  } else if (c->dtype == BPD_BF16) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 16, false>), grid, dim3(256), 0, s, bp);
-  else if (D == 16) hipLaunchKernelGGL((block_bounds_kernel<float, 16, false>), grid, dim3(256), 0, s, bp);
-  else if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<float, 64, false>), grid, dim3(256), 0, s, bp);
-  else hipLaunchKernelGGL((block_bounds_kernel<float, 128, false>), grid, dim3(256), 0, s, bp);
-  hipLaunchKernelGGL(block_pick_kernel, dim3(T, p.kv, B), dim3(PICK_T), 0, s, bp);
+  choose_blocks(*c, bound_args(p, *c, *blocks, chosen, (double*)((char*)workspace + plan.score_at)), s);
   attend<true>(*c, p, plan, s);
   return launched("bpd_sparse_attention");
 }

@@ -22,6 +22,8 @@ struct TreeP {
   int B, T, H, kv, G, cap;                       // cap: rows per sequence
   const int* length; const int* parent;          // parent null: a chain
   float scale, sign;                             // |scale| log2(e) (1 for a scale of 0), and the scale's sign (0)
+  // the decoder's own steps: slots of sequences (cache and summaries of sequence seq[b], -1: none), a tree in a word for all, results as packed_at() of so many columns
+  const int* seq; unsigned long long tree; int packed;
   int nsplit; float* part;                       // parts of the keys, and their results
   int q_f32, o_f32, vec;                         // vec: rows of q and out are 16-byte aligned
   // chosen blocks (null: the whole prefix): bits [b][kv head][node][words], blocks of `bg` groups of 32 keys
@@ -31,13 +33,14 @@ struct TreeP {
 typedef unsigned long long mask64;
 
 // Ancestors of node `lane` (bits), and whether it is there, by all 64 lanes of a wave: after round n a node knows 2^n of its ancestors.
-__device__ __forceinline__ void tree_ancestors(const int* parent, int T, int there, int lane, mask64& anc, bool& ok) {
-  if (!parent) {                                 // a chain
+__device__ __forceinline__ void tree_ancestors(const TreeP& tp, int b, int there, int lane, mask64& anc, bool& ok) {
+  if (!tp.parent && !tp.tree) {                  // a chain
     ok = lane < there;
     anc = ok ? (~0ull >> (63 - lane)) : 0ull;
     return;
   }
-  int p = lane < T ? parent[lane] : -2;
+  int p = -2;
+  if (lane < tp.T) p = tp.parent ? tp.parent[(long)b * tp.T + lane] : (lane ? tree_parent(tp.tree, lane) : -1);
   int good = lane < there && p >= -1 && p < lane;
   if (!good) p = -1;
   unsigned lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
@@ -54,16 +57,18 @@ __device__ __forceinline__ void tree_ancestors(const int* parent, int T, int the
   anc = good ? ((mask64)hi << 32 | lo) : 0ull;
 }
 
-// Rows committed and drafted that the cache holds
+// Whose cache a sequence (or slot) has, and rows committed and drafted that it holds
+__device__ __forceinline__ int tree_cache(const TreeP& p, int b) { const int s = p.seq ? p.seq[b] : b; return s < 0 ? 0 : s; }
 __device__ __forceinline__ void tree_extent(const TreeP& p, int b, int& len, int& there) {
   len = p.length[b];
+  if (p.seq && p.seq[b] < 0) len = -1;
   there = len < 0 ? 0 : (len >= p.cap ? 0 : (p.T < p.cap - len ? p.T : p.cap - len));
   len = len < 0 ? 0 : (len > p.cap ? p.cap : len);
 }
 
 // Four results of a row
 __device__ __forceinline__ void tree_store4(const TreeP& p, int b, int node, int h, int c, const f32x4& v) {
-  const long at = (long)b * p.o_seq + (long)node * p.o_row + (long)h * p.o_head + c;
+  const long at = p.packed ? (long)packed_at((long)b * p.T + node, h * (int)p.o_head + c, p.packed) : (long)b * p.o_seq + (long)node * p.o_row + (long)h * p.o_head + c;
   if (p.o_f32) {
     float* o = (float*)p.out + at;
     if (p.vec) *(f32x4*)o = v; else { o[0] = v[0]; o[1] = v[1]; o[2] = v[2]; o[3] = v[3]; }
@@ -287,8 +292,9 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
   const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, R = p.T * p.G;
   const long pair = (long)b * p.kv + hk;
-  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + (size_t)pair * p.cap * D) + lane;
-  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + (size_t)pair * p.cap * D) + lane;
+  const size_t own = ((size_t)tree_cache(p, b) * p.kv + hk) * p.cap * D;
+  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + own) + lane;
+  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + own) + lane;
   u32x4 kf[2 * KS], kn[2 * KS], vf[VT];
   auto load_k = [&](u32x4 (&k)[2 * KS], int g) {
 #pragma unroll
@@ -299,7 +305,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
   int len, there;
   tree_extent(p, b, len, there);
   mask64 anc; bool ok;
-  tree_ancestors(p.parent ? p.parent + (long)b * p.T : nullptr, p.T, there, lane, anc, ok);
+  tree_ancestors(p, b, there, lane, anc, ok);
   const mask64 present = __ballot(ok);
   mask64 seen[MT]; int node[MT]; bool row_ok[MT];
   bf16x8 qh[Q_LDS ? 1 : MT][KS], ql[QF32 ? MT : 1][KS];
@@ -428,7 +434,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
   int len, there;
   tree_extent(p, b, len, there);
   mask64 anc; bool ok;
-  tree_ancestors(p.parent ? p.parent + (long)b * p.T : nullptr, p.T, there, lane, anc, ok);
+  tree_ancestors(p, b, there, lane, anc, ok);
   const mask64 present = __ballot(ok);
   mask64 seen[MT]; int node[MT]; bool row_ok[MT];
   bf16x8 qh[MT][KS], ql[QF32 ? MT : 1][KS];
@@ -451,8 +457,9 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
     it.n = it.listed + ngr - it.tail0;
   }
   const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
-  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + (size_t)pair * p.cap * D);
-  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + (size_t)pair * p.cap * D);
+  const size_t own = ((size_t)tree_cache(p, b) * p.kv + hk) * p.cap * D;
+  const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + own);
+  const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + own);
   TreeTiles<D, MT, QF32> tiles;
   tiles.clear();
   u32x4 kvn[PER];                                // (a wave's pieces are all of K or all of V)
@@ -519,9 +526,8 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   const int R = p.T * p.G, r0 = rb * 16;
   int len, there;
   tree_extent(p, b, len, there);
-  const int* parent = p.parent ? p.parent + (long)b * p.T : nullptr;
   mask64 anc; bool ok;
-  tree_ancestors(parent, p.T, there, lane, anc, ok);
+  tree_ancestors(p, b, there, lane, anc, ok);
   const mask64 present = __ballot(ok);
   const int row = r0 + lr, node = row < R ? row / p.G : 0;
   mask64 seen = (mask64)(unsigned)__shfl((int)(anc >> 32), node, 64) << 32 | (unsigned)__shfl((int)anc, node, 64);
@@ -547,8 +553,9 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   }
   const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
   const long stride = (long)p.kv * D;
-  const S* Kb = (const S*)p.K + (long)b * p.cap * stride + hk * D;
-  const S* Vb = (const S*)p.V + (long)b * p.cap * stride + hk * D;
+  const long own = (long)tree_cache(p, b) * p.cap * stride + hk * D;
+  const S* Kb = (const S*)p.K + own;
+  const S* Vb = (const S*)p.V + own;
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 acc[VT];
 #pragma unroll

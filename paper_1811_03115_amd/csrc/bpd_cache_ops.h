@@ -108,7 +108,7 @@ struct BoundP {
   TreeP t;
   void* summaries; int tiles;                    // 64 blocks each
   int block, first, recent, top;
-  const int* added;                              // rows behind which the summaries are still those of the last call (null: all are made anew)
+  const int* added; int added_all;               // rows behind which the summaries are still those of the last call; null: added_all for each (< 0: all are made anew)
   double* score;                                 // [b][kv head][node][64 tiles]
   unsigned* chosen;                              // [b][kv head][node][words]
 };
@@ -128,9 +128,10 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
   tree_extent(p.t, b, len, there);
   const int done = len / p.block, blk0 = 64 * tile;
   if (blk0 >= done) return;
-  S* sum = (S*)p.summaries + (((size_t)b * p.t.kv + hk) * p.tiles + tile) * (2 * D * 64);
+  const size_t own = tree_cache(p.t, b);
+  S* sum = (S*)p.summaries + ((own * p.t.kv + hk) * p.tiles + tile) * (2 * D * 64);
   // blocks that the last rows have touched
-  int from = 0;
+  int from = p.added_all < 0 ? 0 : max(0, len - p.added_all) / p.block;
   if (p.added) { const int n = p.added[b]; from = n < 0 ? done : (n >= len ? 0 : (len - n) / p.block); }
   const int f0 = max(from, blk0), f1 = min(done, blk0 + 64);
   for (int blk = f0; blk < f1; ++blk) {
@@ -144,8 +145,8 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
     for (int r = rr; r < p.block; r += PER) {
       const int key = blk * p.block + r;
       const S* k;
-      if constexpr (GROUPED) k = (const S*)p.t.K + ((size_t)b * p.t.kv + hk) * p.t.cap * D + k_at<D>(key, 8 * w);
-      else k = (const S*)p.t.K + ((size_t)b * p.t.cap + key) * p.t.kv * D + (size_t)hk * D + 8 * w;
+      if constexpr (GROUPED) k = (const S*)p.t.K + (own * p.t.kv + hk) * p.t.cap * D + k_at<D>(key, 8 * w);
+      else k = (const S*)p.t.K + (own * p.t.cap + key) * p.t.kv * D + (size_t)hk * D + 8 * w;
 #pragma unroll
       for (int j = 0; j < 8; ++j) { const float v = to_f<S>(k[j]); mn[j] = fminf(mn[j], v); mx[j] = fmaxf(mx[j], v); }
     }
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
   tree_extent(t, b, len, there);
   if (wave == 0) {
     mask64 anc; bool ok;
-    tree_ancestors(t.parent ? t.parent + (long)b * t.T : nullptr, t.T, there, lane, anc, ok);
+    tree_ancestors(t, b, there, lane, anc, ok);
     const mask64 all = __ballot(ok);
     if (lane == 0) ok_s = all;
   }
@@ -358,6 +359,48 @@ __device__ __forceinline__ int accept_walk(const AcceptP& p, int b, int lane, in
   next = want;
   return n;
 }
+// Rows len + path_s[m] of one layer's (sequence, head) to len + m, for m < n, sixteen at a time: read, then written.  (Nodes come in order, path_s[m] >= m: what a batch
+// writes is read by none that follows, and its barrier stands between its writes and the reads before.)
+template <typename S, int D, bool GROUPED>
+__device__ __forceinline__ void accept_move(S* K, S* V, int b, int h, int kv, int cap, int len, int n, const int* path_s, int tid) {
+  constexpr int M = 16, KP = (M * D / 8 + 255) / 256, VP = M * D / 256;
+  if constexpr (GROUPED) { K += ((size_t)b * kv + h) * cap * D; V += ((size_t)b * kv + h) * cap * D; }
+  else { const size_t at = ((size_t)b * cap + len) * kv * D + (size_t)h * D; K += at; V += at; }
+  for (int m0 = 0; m0 < n; m0 += M) {
+    u32x4 k[GROUPED ? KP : 1]; S ke[GROUPED ? 1 : VP], v[VP];
+    if constexpr (GROUPED) {
+#pragma unroll
+      for (int x = 0; x < KP; ++x) {
+        const int e = x * 256 + tid, m = m0 + e / (D / 8), c = e % (D / 8) * 8;
+        if (e < M * D / 8 && m < n && path_s[m] != m) k[x] = *(const u32x4*)(K + k_at<D>(len + path_s[m], c));
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = m0 + e / D, c = e % D;
+      if (m < n && path_s[m] != m) {
+        if constexpr (GROUPED) v[x] = V[v_at<D>(len + path_s[m], c)];
+        else { const size_t s = (size_t)path_s[m] * kv * D + c; ke[x] = K[s]; v[x] = V[s]; }
+      }
+    }
+    __syncthreads();
+    if constexpr (GROUPED) {
+#pragma unroll
+      for (int x = 0; x < KP; ++x) {
+        const int e = x * 256 + tid, m = m0 + e / (D / 8), c = e % (D / 8) * 8;
+        if (e < M * D / 8 && m < n && path_s[m] != m) *(u32x4*)(K + k_at<D>(len + m, c)) = k[x];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < VP; ++x) {
+      const int e = x * 256 + tid, m = m0 + e / D, c = e % D;
+      if (m < n && path_s[m] != m) {
+        if constexpr (GROUPED) V[v_at<D>(len + m, c)] = v[x];
+        else { const size_t s = (size_t)m * kv * D + c; K[s] = ke[x]; V[s] = v[x]; }
+      }
+    }
+  }
+}
 template <typename S, int D, bool GROUPED>
 __global__ __launch_bounds__(256) void tree_accept_kernel(AcceptP p) {
   __shared__ int path_s[TREE_MAX];
@@ -377,46 +420,16 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(AcceptP p) {
   __syncthreads();
   const int n = n_s;
   if (!p.K || n == 0 || path_s[n - 1] == n - 1) return;          // (nodes come in order: then none has moved)
-  S *K = (S*)p.K + (size_t)layer * p.layer, *V = (S*)p.V + (size_t)layer * p.layer;
-  if constexpr (GROUPED) {
-    K += ((size_t)b * p.kv + h) * p.cap * D; V += ((size_t)b * p.kv + h) * p.cap * D;
-    constexpr int KP = TREE_MAX * D / 8 / 256, VP = TREE_MAX * D / 256;
-    u32x4 k[KP]; S v[VP];
-#pragma unroll
-    for (int x = 0; x < KP; ++x) {
-      const int e = x * 256 + tid, m = e / (D / 8), c = e % (D / 8) * 8;
-      if (m < n && path_s[m] != m) k[x] = *(const u32x4*)(K + k_at<D>(len + path_s[m], c));
-    }
-#pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int e = x * 256 + tid, m = e / D, c = e % D;
-      if (m < n && path_s[m] != m) v[x] = V[v_at<D>(len + path_s[m], c)];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < KP; ++x) {
-      const int e = x * 256 + tid, m = e / (D / 8), c = e % (D / 8) * 8;
-      if (m < n && path_s[m] != m) *(u32x4*)(K + k_at<D>(len + m, c)) = k[x];
-    }
-#pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int e = x * 256 + tid, m = e / D, c = e % D;
-      if (m < n && path_s[m] != m) V[v_at<D>(len + m, c)] = v[x];
-    }
-  } else {
-    constexpr int VP = (TREE_MAX * D + 255) / 256;
-    S k[VP], v[VP];
-    const size_t at = ((size_t)b * p.cap + len) * p.kv * D + (size_t)h * D;
-#pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int e = x * 256 + tid, m = e / D, c = e % D;
-      if (m < n && path_s[m] != m) { const size_t s = at + (size_t)path_s[m] * p.kv * D + c; k[x] = K[s]; v[x] = V[s]; }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < VP; ++x) {
-      const int e = x * 256 + tid, m = e / D, c = e % D;
-      if (m < n && path_s[m] != m) { const size_t s = at + (size_t)m * p.kv * D + c; K[s] = k[x]; V[s] = v[x]; }
-    }
-  }
+  accept_move<S, D, GROUPED>((S*)p.K + (size_t)layer * p.layer, (S*)p.V + (size_t)layer * p.layer, b, h, p.kv, p.cap, len, n, path_s, tid);
+}
+// The same for a path that has been found already: accepted[b] nodes path[b * ld ..], length[b] with them
+struct MoveP { const int *path, *accepted, *length; int ld; void *K, *V; long layer; int kv, cap; };
+template <typename S, int D, bool GROUPED>
+__global__ __launch_bounds__(256) void tree_move_kernel(MoveP p) {
+  __shared__ int path_s[TREE_MAX];
+  const int tid = threadIdx.x, h = blockIdx.x, layer = blockIdx.y, b = blockIdx.z, n = min(p.accepted[b], p.ld);
+  if (tid < n) path_s[tid] = p.path[(long)b * p.ld + tid];
+  __syncthreads();
+  if (n <= 0 || path_s[n - 1] == n - 1) return;
+  accept_move<S, D, GROUPED>((S*)p.K + (size_t)layer * p.layer, (S*)p.V + (size_t)layer * p.layer, b, h, p.kv, p.cap, p.length[b] - n, n, path_s, tid);
 }

@@ -64,3 +64,18 @@ __device__ __forceinline__ float wave_sum(float v) {
   v += dpp_move<0x140>(v);                       // row_mirror
   return sum_rows(v);
 }
+
+// Element (m, c) of activations [rows][K] as row_gemm_kernel reads them: the operands of its matrix instructions one behind the other, [row tile][k-step of 32][lane][8], whole row tiles.  (Taken
+// as operands out of rows in memory, a load of 1 KB touches 64 lines, which the L1 looks up one by one: 64 cycles instead of 16: the queries, keys
+// and values of 320 x 1024 10.6 us, packed 8.3, their first FFN layer 12.8, 9.8, an output projection 6.8, 5.9;  170 rows 8.9, 7.3;  8.5, 6.4;  5.3, 5.1.)
+__device__ __forceinline__ size_t packed_at(long m, int c, int K) {
+  return (size_t)(m & ~15l) * K + (c >> 5) * 512 + ((c >> 3) & 3) * 128 + (int)(m & 15) * 8 + (c & 7);
+}
+
+// A tree of up to 16 nodes in a word: four bits a node, its parent (of node 0, which follows the prefix, 15: the word is not 0, which stands for a chain)
+__device__ __forceinline__ int tree_parent(unsigned long long tree, int i) { return (int)(tree >> (4 * i) & 15); }
+__device__ __forceinline__ int tree_depth(unsigned long long tree, int i) {
+  int e = 0;
+  for (; i > 0; ++e) i = tree_parent(tree, i);   // (a parent comes before its children)
+  return e;
+}

@@ -444,10 +444,11 @@ __global__ __launch_bounds__(64) void fold_layernorm_kernel(const bf16_t* Wp, bf
 //   x[row][c] = sqrt(d) * E[tok][c] + pos[position][c];  tok < 0 -> zero vector (the shifted
 //   decoder input at position 0).  E is the packed vocabulary matrix in bf16 mode.
 // seq (decoder side, may be null): the sequence of every slot of rows_per_seq rows (base: indexed by slot), -1: not in use.
+// tree (0: a chain): the rows are the nodes of a tree (tree_parent()), each at the position of its depth.
 template <bool BF16>
 __global__ void embed_kernel(const int* tok, int tok_ld, const int* base, int rows_per_seq, int M,
                              int d, const void* E, int V, const float* pos, float scale, float* x,
-                             int zero_input, unsigned long long* keys, int nkeys, const int* seq) {
+                             int zero_input, unsigned long long* keys, int nkeys, const int* seq, unsigned long long tree) {
   const long idx = (long)blockIdx.x * blockDim.x + threadIdx.x;
   if (idx < nkeys) keys[idx] = 0ull;          // argmax keys of this invocation start at "nothing"
   if (idx >= (long)M * d) return;
@@ -455,7 +456,7 @@ __global__ void embed_kernel(const int* tok, int tok_ld, const int* base, int ro
   const int b = row / rows_per_seq, i = row % rows_per_seq;
   const int q = seq ? seq[b] : b;
   if (q < 0) return;
-  const int position = (base ? base[b] : 0) + i;
+  const int position = (base ? base[b] : 0) + (tree ? tree_depth(tree, i) : i);
   float v = pos[(long)position * d + c];
   if (!zero_input) {
     int t = tok[q * tok_ld + i];
@@ -480,7 +481,7 @@ __global__ void embed_kernel(const int* tok, int tok_ld, const int* base, int ro
 __global__ __launch_bounds__(64) void embed_stats_kernel(const int* tok, int tok_ld, const int* base, int rows_per_seq,
                                                          int M, int d, const bf16_t* E, int V, const float* pos,
                                                          float scale, float* x, int zero_input, float* stats,
-                                                         unsigned long long* keys, int nkeys, const int* seq) {
+                                                         unsigned long long* keys, int nkeys, const int* seq, unsigned long long tree) {
   const int tile = blockIdx.x, lane = threadIdx.x;
   for (int i = tile * 64 + lane; i < nkeys; i += gridDim.x * 64) keys[i] = 0ull;
   const int row = lane & 15, c0 = tile * 16 + (lane >> 4) * 4;
@@ -488,7 +489,7 @@ __global__ __launch_bounds__(64) void embed_stats_kernel(const int* tok, int tok
   const int b = r / rows_per_seq, i = r % rows_per_seq;
   int sq = seq ? seq[b] : b;
   sq = sq < 0 ? 0 : sq;                          // (a slot not in use, of length 0: any row will do)
-  const int position = (base ? base[b] : 0) + i;
+  const int position = (base ? base[b] : 0) + (tree ? tree_depth(tree, i) : i);
   const float4 pv = *(const float4*)(pos + (long)position * d + c0);
   float v[4] = {pv.x, pv.y, pv.z, pv.w};
   if (!zero_input) {
@@ -661,12 +662,6 @@ template <int DH> struct RowLoader<bf16_t, DH> {
   }
 };
 
-// Element (m, c) of activations [rows][K] as row_gemm_kernel reads them: the operands of its matrix instructions one behind the other, [row tile][k-step of 32][lane][8], whole row tiles.  (Taken
-// as operands out of rows in memory, a load of 1 KB touches 64 lines, which the L1 looks up one by one: 64 cycles instead of 16: the queries, keys
-// and values of 320 x 1024 10.6 us, packed 8.3, their first FFN layer 12.8, 9.8, an output projection 6.8, 5.9;  170 rows 8.9, 7.3;  8.5, 6.4;  5.3, 5.1.)
-__device__ __forceinline__ size_t packed_at(long m, int c, int K) {
-  return (size_t)(m & ~15l) * K + (c >> 5) * 512 + ((c >> 3) & 3) * 128 + (int)(m & 15) * 8 + (c & 7);
-}
 struct AttnP {
   // (what the first loads need comes first: one scalar load)
   const void* Kc; const void* Vc;
@@ -1247,6 +1242,29 @@ __global__ __launch_bounds__(64) void accept_kernel(StateP s, const unsigned lon
   }
 }
 
+// Slots of this step (sequences not ended before step live_step - 1) and of the next (not before this one), by one wave: sequence b's in slot_s (LDS; -1: none), and the next
+// step's dealt.  (The workgroups of this launch write fin_step too: live_step, which both tests let pass.)
+__device__ __forceinline__ void deal_slots(const StateP& s, int b, int B, int lane, int live_step, int* slot_s) {
+  int cur = 0, nxt = 0, all_cur = 0, all_nxt = 0, mine = 0;
+  for (int q0 = 0; q0 < B; q0 += 64) {
+    const int q = q0 + lane, f = q < B ? s.fin_step[q] : -2;
+    const unsigned long long bc = __ballot(f >= live_step - 1), bn = __ballot(f >= live_step);
+    const unsigned long long below = b >= q0 + 64 ? ~0ull : (b > q0 ? (1ull << (b - q0)) - 1ull : 0ull);
+    cur += __popcll(bc & below); nxt += __popcll(bn & below);
+    all_cur += __popcll(bc); all_nxt += __popcll(bn);
+    if (b >= q0 && b < q0 + 64) mine = (int)((bc >> (b - q0)) & 1) | ((int)((bn >> (b - q0)) & 1) << 1);
+  }
+  if (lane == 0) {
+    slot_s[0] = mine & 1 ? cur : -1; slot_s[1] = mine & 2 ? nxt : -1;
+    if (mine & 2) { s.slot_seq[nxt] = b; s.slot_src[nxt] = s.src_len[b]; }
+    else if (mine & 1) {                       // leaves: the last slots, as many as sequences leave, fall free
+      const int q = all_nxt + cur - nxt;
+      s.slot_seq[q] = -1; s.slot_L[q] = 0; s.slot_row[q] = b * s.cache_rows + s.L[b];
+    }
+    if (b == 0) *s.n_live = all_nxt;
+  }
+}
+
 // accept_kernel followed, in the same launch, by the embedding of the next block (embed_stats_kernel; bf16, d <= 1024):
 // the step is a chain of dependent kernels and each one saved counts.  One
 // workgroup of 16 waves per sequence: wave 0 verifies / accepts / commits, then every wave embeds four 16-column tiles of
@@ -1271,28 +1289,9 @@ __global__ __launch_bounds__(1024) void accept_embed_kernel(StateP s, unsigned l
   if (b >= B) return;
   const int live_step = s.steps_done[b], tick = s.dyn ? s.tick[b] : 0;      // (the same for every sequence: each launch moves all on by one)
   if (s.dyn) step_from_dyn(s, tick);
-  // Slots of this step (sequences not ended before step live_step - 1) and of the next (not before this one).  (The
-  // workgroups of this launch write fin_step too: live_step, which both tests let pass.)  With all of the batch in this
-  // step (slots == 1) the slot is the sequence and only the next step's is worked out, by a wave of its own.
+  // With all of the batch in this step (slots == 1) the slot is the sequence and only the next step's is worked out, by a wave of its own.
   if (slots && wave == (slots == 1 ? 1 : 0)) {
-    int cur = 0, nxt = 0, all_cur = 0, all_nxt = 0, mine = 0;
-    for (int q0 = 0; q0 < B; q0 += 64) {
-      const int q = q0 + lane, f = q < B ? s.fin_step[q] : -2;
-      const unsigned long long bc = __ballot(f >= live_step - 1), bn = __ballot(f >= live_step);
-      const unsigned long long below = b >= q0 + 64 ? ~0ull : (b > q0 ? (1ull << (b - q0)) - 1ull : 0ull);
-      cur += __popcll(bc & below); nxt += __popcll(bn & below);
-      all_cur += __popcll(bc); all_nxt += __popcll(bn);
-      if (b >= q0 && b < q0 + 64) mine = (int)((bc >> (b - q0)) & 1) | ((int)((bn >> (b - q0)) & 1) << 1);
-    }
-    if (lane == 0) {
-      slot_s[0] = mine & 1 ? cur : -1; slot_s[1] = mine & 2 ? nxt : -1;
-      if (mine & 2) { s.slot_seq[nxt] = b; s.slot_src[nxt] = s.src_len[b]; }
-      else if (mine & 1) {                       // leaves: the last slots, as many as sequences leave, fall free
-        const int q = all_nxt + cur - nxt;
-        s.slot_seq[q] = -1; s.slot_L[q] = 0; s.slot_row[q] = b * s.cache_rows + s.L[b];
-      }
-      if (b == 0) *s.n_live = all_nxt;
-    }
+    deal_slots(s, b, B, lane, live_step, slot_s);
   }
   int slot = b;
   if (slots == 2) {
@@ -1405,6 +1404,75 @@ __global__ __launch_bounds__(1024) void accept_embed_kernel(StateP s, unsigned l
     }
   }
   if (stats && per_block && 4 * wave < ntiles && lane < 16 && i < k) ((float2*)stats)[(long)wave * srows + row] = make_float2(bs, bq);
+}
+
+// accept_kernel for a block whose rows are the nodes of a tree: the first node is taken (it is p_1's own choice), then, as long as there is one, the first child of the last
+// accepted node whose token is p_1's arg-max there; cut at the first EOS and at max_len.  path[b][kmax]: the accepted nodes (tree_move_kernel moves their cache rows).
+// Next proposals: node i, at depth e and the r-th of its siblings, gets what the table says about its position: head e + r + 1 at the accepted node r before the last one
+// (the paper's step makes all k x k arg-maxes and uses one row; the others are other opinions about the same positions), or where there is none head e + 1 at the last.
+// slots != 0: the next step's slots are dealt here, as accept_embed_kernel does.
+__global__ __launch_bounds__(64) void accept_tree_kernel(StateP s, const unsigned long long* keys, int k, int B, unsigned long long tree, int* accepted_out, int* path, int slots) {
+  __shared__ int slot_s[2];
+  __shared__ int A_s[256];
+  __shared__ int path_s[16];
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const int live_step = s.steps_done[b];
+  if (slots) deal_slots(s, b, B, lane, live_step, slot_s);
+  int Ln = s.L[b];
+  if (s.finished[b]) {
+    if (lane == 0) { s.accepted[b] = 0; if (accepted_out) accepted_out[b] = 0; }
+  } else {
+    for (int e = lane; e < k * k; e += 64) {
+      const int a = key_index(keys[(long)b * k * k + e]);
+      A_s[e] = a;
+      s.A[(b * s.kmax + e / k) * s.kmax + e % k] = a;
+    }
+    __syncthreads();
+    const int tok = lane < k ? s.P[b * s.kmax + lane] : -1, up = lane > 0 && lane < k ? tree_parent(tree, lane) : -1;
+    const int j = s.j[b], room = s.max_len[b] - j;
+    int n = 0, cur = 0, mine = -1;
+    bool eos = false;
+    for (;;) {                                   // (the same for the whole wave; at most k rounds: nodes come behind their parents)
+      if (lane == n) mine = cur;
+      ++n;
+      const int t = __shfl(tok, cur, 64);
+      eos = s.eos_id >= 0 && t == s.eos_id;
+      if (eos || n >= room) break;
+      const unsigned long long m = __ballot(up == cur && tok == A_s[cur * k]);
+      if (!m) break;
+      cur = __ffsll((long long)m) - 1;
+    }
+    if (lane < k) { path_s[lane] = mine; path[b * s.kmax + lane] = mine; }
+    const int said = __shfl(tok, mine < 0 ? 0 : mine, 64);
+    if (lane < n) s.out_ids[(long)b * s.max_out + j + lane] = said;
+    __syncthreads();
+    if (lane < k) {
+      const int e = tree_depth(tree, lane);
+      int r = 0;
+      for (int q = 1; q < lane; ++q) r += lane > 0 && tree_parent(tree, q) == up;
+      if (n - 1 - r < 0 || e + r >= k) r = 0;
+      s.P[b * s.kmax + lane] = A_s[path_s[n - 1 - r] * k + e + r];
+    }
+    Ln += n;
+    if (lane == 0) {
+      const int fin = eos || j + n >= s.max_len[b];
+      s.j[b] = j + n;
+      s.L[b] = Ln;
+      s.finished[b] = fin;
+      if (fin) s.fin_step[b] = live_step;
+      s.accepted[b] = n;
+      if (accepted_out) accepted_out[b] = n;
+      atomicAdd((unsigned long long*)&s.stats[0], 1ull);
+      atomicAdd((unsigned long long*)&s.stats[1], (unsigned long long)n);
+      if (fin) atomicAdd((unsigned long long*)&s.stats[2], 1ull);
+      atomicAdd((unsigned long long*)&s.stats[3 + n], 1ull);
+      atomicMax((unsigned long long*)&s.stats[20], (unsigned long long)(live_step + 1));   // steps with a live sequence
+    }
+  }
+  if (lane == 0) {
+    s.steps_done[b] = live_step + 1;
+    if (slots && slot_s[1] >= 0) { s.slot_L[slot_s[1]] = Ln; s.slot_row[slot_s[1]] = b * s.cache_rows + Ln; }
+  }
 }
 
 #include "bpd_small.h"
