@@ -49,7 +49,7 @@ RowsP rows_of(const bpd_rows& r) { return RowsP{r.data, r.dtype == BPD_F32, rows
 
 template <int D, int MT, int NW, bool SPARSE>
 void attend_few(const TreeP& p, hipStream_t s) {
-  const dim3 grid(p.nsplit, p.kv, p.B);
+  const dim3 grid(p.parts, p.kv);
   if constexpr (MT <= 2) {                       // (queries of fp32 and of many rows take other tiles: attend_groups)
     if (p.q_f32) { hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, true, SPARSE>), grid, dim3(64 * NW), 0, s, p); return; }
   }
@@ -59,40 +59,37 @@ template <int D, bool SPARSE>
 void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
   const int R = p.T * p.G;
   if (plan.rows || (p.q_f32 && R > 32)) {
-    if (p.q_f32) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 8, true, SPARSE>), dim3(p.nsplit * ((R + 127) / 128), p.kv, p.B), dim3(512), 0, s, p);
-    else if (plan.waves == 4) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.nsplit * plan.blocks, p.kv, p.B), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 8, false, SPARSE>), dim3(p.nsplit * plan.blocks, p.kv, p.B), dim3(512), 0, s, p);
-  } else if (plan.mt == 1) {
-    if (plan.waves == 4) attend_few<D, 1, 4, SPARSE>(p, s);
-    else attend_few<D, 1, 8, SPARSE>(p, s);
-  } else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
-  else if (plan.mt == 3) attend_few<D, 3, 4, SPARSE>(p, s);
-  else attend_few<D, 4, 4, SPARSE>(p, s);
-}
-template <int D, int NG>
-void join_of(const TreeP& p, hipStream_t s) {
-  const long rows = (long)p.B * p.kv * p.T * p.G, per = 256 / (D / 4 * NG);
-  hipLaunchKernelGGL((tree_join_kernel<D, NG>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, p);
+    if (p.q_f32) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, true, SPARSE>), dim3(p.parts * ((R + 63) / 64), p.kv), dim3(256), 0, s, p);
+    else if (plan.mt == 1) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
+  } else if (plan.mt == 1) attend_few<D, 1, 4, SPARSE>(p, s);
+  else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
+  else if constexpr (D == 64) { if (plan.mt == 3) attend_few<D, 3, 4, SPARSE>(p, s); else attend_few<D, 4, 4, SPARSE>(p, s); }
+
 }
 template <int D>
-void join(const TreeP& p, hipStream_t s) {       // (threads for every fourth, or eighth, split)
-  if (p.nsplit <= 4) join_of<D, 1>(p, s);
-  else if (p.nsplit <= 16) join_of<D, 4>(p, s);
-  else join_of<D, 8>(p, s);
+void join(const TreeP& p, hipStream_t s) {
+  const long rows = (long)p.B * p.kv * p.T * p.G;
+  // a wave has D / 4 lanes per part: more than eight rounds of that, and few rows, are for four waves
+  if (p.nsplit > 8 * 256 / D && rows < 4096) hipLaunchKernelGGL((tree_join_kernel<D, 4>), dim3((unsigned)rows), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((tree_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
 }
 template <bool SPARSE>
-void attend(const bpd_cache& c, const TreeP& p, const TreePlan& plan, hipStream_t s) {
+void attend(const bpd_cache& c, const TreeP& args, const TreePlan& plan, hipStream_t s) {
   const int D = c.head_dim;
+  TreeP p = args;
+  // (by length: a lane knows one sequence's; its sums cost some 1 us, which short caches do not have; chosen blocks are about as many in every sequence)
+  p.nsplit = plan.nsplit; p.parts = p.B * plan.nsplit; p.by_length = !SPARSE && plan.nsplit > 1 && p.B > 1 && p.B <= 64 && c.capacity >= 4096;
   if (cache_grouped(c)) {
     if (D == 64) attend_groups<64, SPARSE>(p, plan, s); else attend_groups<128, SPARSE>(p, plan, s);
   } else {
-    const dim3 grid(p.nsplit * plan.blocks, p.kv, p.B);
+    const dim3 grid(p.parts * plan.blocks, p.kv);
     if (c.dtype == BPD_BF16) hipLaunchKernelGGL((tree_rows_kernel<bf16_t, 16, SPARSE>), grid, dim3(256), 0, s, p);
     else if (D == 16) hipLaunchKernelGGL((tree_rows_kernel<float, 16, SPARSE>), grid, dim3(256), 0, s, p);
     else if (D == 64) hipLaunchKernelGGL((tree_rows_kernel<float, 64, SPARSE>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((tree_rows_kernel<float, 128, SPARSE>), grid, dim3(256), 0, s, p);
   }
-  if (p.nsplit > 1) { if (D == 16) join<16>(p, s); else if (D == 64) join<64>(p, s); else join<128>(p, s); }
+  if (p.parts > p.B) { if (D == 16) join<16>(p, s); else if (D == 64) join<64>(p, s); else join<128>(p, s); }
 }
 
 // Bounds of the blocks, with fresh summaries (no nodes: those alone), and the blocks that each node sees
@@ -158,7 +155,6 @@ void launch_block_attention(const BlockAttention& a, hipStream_t stream) {
   p.part = (float*)a.scratch;
   const size_t one = (size_t)a.B * c.n_kv_heads * a.T * (dh + 2) * 4;           // bytes of one part of the keys
   if (!block && plan.nsplit > 1 && plan.nsplit * one > a.scratch_bytes) plan.nsplit = (int)(a.scratch_bytes / one) > 1 ? (int)(a.scratch_bytes / one) : 1;
-  p.nsplit = plan.nsplit;
   if (!block || c.capacity < block) { attend<false>(c, p, plan, stream); return; }
   BoundP bp = bound_args(p, c, *a.blocks, (unsigned*)((char*)a.scratch + plan.chosen_at), (double*)((char*)a.scratch + plan.score_at));
   bp.added_all = a.added;
@@ -231,7 +227,7 @@ int bpd_tree_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* ou
   const TreePlan plan = plan_attention(*c, B, T, heads, 0, compute_units());
   if (plan.bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < plan.bytes)) return refuse(BPD_E_CAPACITY, "bpd_tree_attention: workspace too small or not aligned to 16 bytes");
   TreeP p = attention_args(*c, *q, *out, length, parent, B, T, heads, scale);
-  p.nsplit = plan.nsplit; p.part = (float*)workspace;
+  p.part = (float*)workspace;
   attend<false>(*c, p, plan, (hipStream_t)hip_stream);
   return launched("bpd_tree_attention");
 }
@@ -250,7 +246,7 @@ int bpd_sparse_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* 
   if (plan.bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < plan.bytes)) return refuse(BPD_E_CAPACITY, "bpd_sparse_attention: workspace too small or not aligned to 16 bytes");
   const hipStream_t s = (hipStream_t)hip_stream;
   TreeP p = attention_args(*c, *q, *out, length, parent, B, T, heads, scale);
-  p.nsplit = plan.nsplit; p.part = (float*)workspace;
+  p.part = (float*)workspace;
   if (nb == 0) {                                 // nothing to choose from
     attend<false>(*c, p, plan, s);
     return launched("bpd_sparse_attention");

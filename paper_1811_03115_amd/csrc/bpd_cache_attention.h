@@ -24,7 +24,8 @@ struct TreeP {
   float scale, sign;                             // |scale| log2(e) (1 for a scale of 0), and the scale's sign (0)
   // the decoder's own steps: slots of sequences (cache and summaries of sequence seq[b], -1: none), a tree in a word for all, results as packed_at() of so many columns
   const int* seq; unsigned long long tree; int packed;
-  int nsplit; float* part;                       // parts of the keys, and their results
+  // parts of the keys: `parts` in all of each key head's sequences, nsplit of each sequence, or (by_length) as many as its share of the keys; their results
+  int nsplit, parts, by_length; float* part;
   int q_f32, o_f32, vec;                         // vec: rows of q and out are 16-byte aligned
   // chosen blocks (null: the whole prefix): bits [b][kv head][node][words], blocks of `bg` groups of 32 keys
   const unsigned* chosen; int words, bg;
@@ -64,6 +65,37 @@ __device__ __forceinline__ void tree_extent(const TreeP& p, int b, int& len, int
   if (p.seq && p.seq[b] < 0) len = -1;
   there = len < 0 ? 0 : (len >= p.cap ? 0 : (p.T < p.cap - len ? p.T : p.cap - len));
   len = len < 0 ? 0 : (len > p.cap ? p.cap : len);
+}
+
+// The sequence that a part belongs to, its number among that sequence's parts, how many those are and where they begin.  By length (up to 64 sequences, a lane each): one part each,
+// and the others as the keys are spread.  (Eight documents of 8000 .. 32000 keys in equal numbers of parts: the longest one's decide.)
+struct TreePart { int b, split, n, first; };
+__device__ __forceinline__ void tree_shares(const TreeP& p, int lane, int& n, int& end) {
+  const int len = lane < p.B ? p.length[lane] : -1;
+  long items = len < 0 ? 0 : (min(len, p.cap) + p.T + 31) >> 5, all = items;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, 64);
+  n = lane < p.B ? 1 + (all ? (int)((long)(p.parts - p.B) * items / all) : 0) : 0;
+  end = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(end, o, 64); if (lane >= o) end += v; }
+}
+__device__ __forceinline__ TreePart tree_part(const TreeP& p, int at, int lane) {      // (b < 0: nobody's)
+  if (!p.by_length) return TreePart{at / p.nsplit, at % p.nsplit, p.nsplit, at - at % p.nsplit};
+  int n, end;
+  tree_shares(p, lane, n, end);
+  const mask64 mine = __ballot(at >= end - n && at < end);
+  const int b = mine ? __ffsll((long long)mine) - 1 : -1, q = b < 0 ? 0 : b;
+  const int nb = __builtin_amdgcn_readfirstlane(__shfl(n, q, 64)), first = __builtin_amdgcn_readfirstlane(__shfl(end, q, 64)) - nb;
+  return TreePart{__builtin_amdgcn_readfirstlane(b), at - first, nb, first};
+}
+// ... of sequence b, by a wave whose lanes ask for sequences of their own
+__device__ __forceinline__ void tree_parts_of(const TreeP& p, int b, int lane, int& n, int& first) {
+  n = p.nsplit; first = b * p.nsplit;
+  if (!p.by_length) return;
+  int m, end;
+  tree_shares(p, lane, m, end);
+  n = __shfl(m, b, 64); first = __shfl(end, b, 64) - n;
 }
 
 // Four results of a row
@@ -262,11 +294,11 @@ __device__ __forceinline__ void tree_q_operand(const TreeP& p, int b, int hk, in
   for (int j = 0; j < 8; ++j) v[j] *= p.sign;    // (of the scale: the maximum is that of the products)
   tree_pair(v, hi, lo);
 }
-// A row's result or partial result: dimensions c .. c + 3.  Partial results: [pair][split][row][D], then [pair][split][row] maxima and as many sums
-__device__ __forceinline__ void tree_finish4(const TreeP& p, int D, long pair, int b, int hk, int split, int r, int R, int node, int c, float M, float L, const f32x4& o) {
+// A row's result or partial result: dimensions c .. c + 3.  Partial results: [key head][part][row][D], then [key head][part][row] maxima and as many sums
+__device__ __forceinline__ void tree_finish4(const TreeP& p, int D, int b, int hk, int part, int r, int R, int node, int c, float M, float L, const f32x4& o) {
   if (r >= R) return;
-  if (p.nsplit > 1) {
-    const long at = (pair * p.nsplit + split) * R + r, rows = (long)p.B * p.kv * p.nsplit * R;
+  if (p.parts > p.B) {
+    const long at = ((long)hk * p.parts + part) * R + r, rows = (long)p.kv * p.parts * R;
     *(f32x4*)(p.part + at * D + c) = o;
     if (c == 0) { p.part[rows * D + at] = M; p.part[rows * (D + 1) + at] = L; }
   } else {
@@ -280,7 +312,7 @@ __device__ __forceinline__ void tree_finish4(const TreeP& p, int D, long pair, i
 // Up to 64 rows: a workgroup has all of a (sequence, key head) pair's, and one part in nsplit of its items; its NW waves take single items in turn, each with its own
 // maximum, sum and results, and meet once in LDS.  What bounds it is the stream of K and V; the next item's keys are asked for while this one's values are multiplied.
 template <int D, int MT, int NW, bool QF32, bool SPARSE>
-__global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
+__global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
   constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D, SLOTS = NW / 2 > 4 ? NW / 2 : 4;
   constexpr bool Q_LDS = MT * KS > 8 && !QF32;   // queries of many rows: in LDS, for registers
   __shared__ __attribute__((aligned(16))) f32x4 o_s[SLOTS][VT][64];
@@ -290,7 +322,10 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
   static_assert(!Q_LDS || MT * KS <= SLOTS * VT, "queries fit where the results meet");
   u32x4 (*q_s)[KS][64] = (u32x4 (*)[KS][64])&o_s[0][0][0];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
-  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, R = p.T * p.G;
+  const int at_part = blockIdx.x, hk = blockIdx.y, R = p.T * p.G;
+  const TreePart part = tree_part(p, at_part, lane);
+  if (part.b < 0) return;
+  const int b = part.b;
   const long pair = (long)b * p.kv + hk;
   const size_t own = ((size_t)tree_cache(p, b) * p.kv + hk) * p.cap * D;
   const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + own) + lane;
@@ -301,7 +336,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
     for (int x = 0; x < 2 * KS; ++x) k[x] = Kb[(size_t)g * (GRP / 8) + x * 64];
   };
   // with all keys here the first item's keys do not wait for the length
-  if (!SPARSE && p.nsplit == 1) load_k(kf, min(wave, p.cap / 32 - 1));
+  if (!SPARSE && part.n == 1) load_k(kf, min(wave, p.cap / 32 - 1));
   int len, there;
   tree_extent(p, b, len, there);
   mask64 anc; bool ok;
@@ -335,7 +370,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
     it.n = it.listed + ngr - it.tail0;
   }
   if constexpr (Q_LDS) __syncthreads();
-  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
+  const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);
   TreeTiles<D, MT, QF32> tiles;
   tiles.clear();
   int i = i0 + wave, g = i < i1 ? __builtin_amdgcn_readfirstlane(it.group(i)) : 0;
@@ -349,7 +384,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
   };
   if (i < i1) {
     load_words(i, g);
-    if (SPARSE || p.nsplit > 1) load_k(kf, g);
+    if (SPARSE || part.n > 1) load_k(kf, g);
   }
   auto step = [&](u32x4 (&k)[2 * KS], u32x4 (&k_next)[2 * KS]) {
 #pragma unroll
@@ -413,7 +448,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
     __syncthreads();
     for (int x = wave; x < VT; x += NW) {
       const f32x4 o = (o_s[0][x][lane] + o_s[1][x][lane]) + (o_s[2][x][lane] + o_s[3][x][lane]);
-      tree_finish4(p, D, pair, b, hk, split, 16 * t + lr, R, node[t], 16 * x + 4 * lq, M[t], L[t], o);
+      tree_finish4(p, D, b, hk, at_part, 16 * t + lr, R, node[t], 16 * x + 4 * lq, M[t], L[t], o);
     }
     if (t + 1 < MT) __syncthreads();
   }
@@ -422,14 +457,17 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_kernel(TreeP p) {
 // More than 64 rows: the waves have rows of their own, 16 MT each, and walk the same items, which come through LDS, two buffers in turn: an operand is loaded once for 16 MT NW
 // rows.  What bounds it is the matrix cores (6 D products per row and 64 keys, with the pairs) and, beside them, the exponentials.
 template <int D, int MT, int NW, bool QF32, bool SPARSE>
-__global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
+__global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p) {
   constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D, PIECES = 4 * D, PER = 2 * PIECES / (64 * NW);   // 16-byte pieces of K (and of V) in an item; of both per thread
   static_assert(PER >= 1, "");
   __shared__ __attribute__((aligned(16))) u32x4 kv_s[2][2 * PIECES];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
-  const int split = blockIdx.x % p.nsplit, rb = blockIdx.x / p.nsplit, hk = blockIdx.y, b = blockIdx.z, R = p.T * p.G, r0 = (rb * NW + wave) * 16 * MT;
+  const int at_part = blockIdx.x % p.parts, rb = blockIdx.x / p.parts, hk = blockIdx.y, R = p.T * p.G, r0 = (rb * NW + wave) * 16 * MT;
+  const TreePart part = tree_part(p, at_part, lane);
+  if (part.b < 0) return;
+  const int b = part.b;
   const long pair = (long)b * p.kv + hk;
   int len, there;
   tree_extent(p, b, len, there);
@@ -456,7 +494,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
     it.listed = tree_list(picks, p.words, w0 / p.G, (w1 + p.G - 1) / p.G, done, list_s, sums_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
-  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
+  const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);
   const size_t own = ((size_t)tree_cache(p, b) * p.kv + hk) * p.cap * D;
   const u32x4* Kb = (const u32x4*)((const bf16_t*)p.K + own);
   const u32x4* Vb = (const u32x4*)((const bf16_t*)p.V + own);
@@ -507,7 +545,7 @@ __global__ __launch_bounds__(64 * NW) void tree_attention_rows_kernel(TreeP p) {
   for (int t = 0; t < MT; ++t) {
     const float L = sum_rows(tiles.l[t]);
 #pragma unroll
-    for (int x = 0; x < VT; ++x) tree_finish4(p, D, pair, b, hk, split, r0 + 16 * t + lr, R, node[t], 16 * x + 4 * lq, tiles.m[t], L, tiles.acc[t][x]);
+    for (int x = 0; x < VT; ++x) tree_finish4(p, D, b, hk, at_part, r0 + 16 * t + lr, R, node[t], 16 * x + 4 * lq, tiles.m[t], L, tiles.acc[t][x]);
   }
 }
 
@@ -522,8 +560,10 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
-  const int split = blockIdx.x % p.nsplit, rb = blockIdx.x / p.nsplit, hk = blockIdx.y, b = blockIdx.z;
-  const int R = p.T * p.G, r0 = rb * 16;
+  const int at_part = blockIdx.x % p.parts, rb = blockIdx.x / p.parts, hk = blockIdx.y, R = p.T * p.G, r0 = rb * 16;
+  const TreePart part = tree_part(p, at_part, lane);
+  if (part.b < 0) return;
+  const int b = part.b;
   int len, there;
   tree_extent(p, b, len, there);
   mask64 anc; bool ok;
@@ -551,7 +591,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
     it.listed = tree_list(picks, p.words, n0, n1, done, list_s, sums_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
-  const int i0 = (int)((long)it.n * split / p.nsplit), i1 = (int)((long)it.n * (split + 1) / p.nsplit);
+  const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);
   const long stride = (long)p.kv * D;
   const long own = (long)tree_cache(p, b) * p.cap * stride + hk * D;
   const S* Kb = (const S*)p.K + own;
@@ -630,43 +670,44 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
       L = fmaf(l_s[w][lr], a, L);
       o += o_s[w][x][lane] * a;
     }
-    tree_finish4(p, D, (long)b * p.kv + hk, b, hk, split, row, R, node, 16 * x + 4 * lq, M, L, o);
+    tree_finish4(p, D, b, hk, at_part, row, R, node, 16 * x + 4 * lq, M, L, o);
   }
 }
 
-// Partial results of the splits joined:  out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  NG x D / 4 threads per row, each with every NG-th split, that meet in LDS: a
-// chain of three trips to memory whatever the number of splits.
-template <int D, int NG>
+// Partial results of a row's parts joined:  out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).  NW waves per row: their lanes find the maximum, then D / 4 of them at a time
+// take a part each, all of a thread's under way together, and meet in LDS: three trips to memory whatever the number of parts (64 of them, one thread after the other: 33 us;
+// so 5).
+template <int D, int NW>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeP p) {
-  constexpr int Q = D / 4, PER = 256 / (Q * NG);
-  __shared__ __attribute__((aligned(16))) f32x4 o_s[NG > 1 ? 256 : 1];
-  __shared__ float l_s[NG > 1 ? 256 : 1];
-  const int R = p.T * p.G, tid = threadIdx.x, c = tid % Q, ng = tid / Q % NG;
-  const long id = (long)blockIdx.x * PER + tid / (Q * NG), pairs = (long)p.B * p.kv, rows = pairs * p.nsplit * R;
-  const bool live = id < pairs * R;
-  const long pair = live ? id / R : 0;
-  const int r = live ? (int)(id - pair * R) : 0;
-  const long at = pair * p.nsplit * R + r;
+  constexpr int Q = D / 4, NG = 64 * NW / Q;
+  __shared__ __attribute__((aligned(16))) f32x4 o_s[256];
+  __shared__ float l_s[256];
+  const int R = p.T * p.G, tid = threadIdx.x, lane = tid & 63, own = tid % (64 * NW), c = own % Q, ng = own / Q;
+  const long id = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (4 / NW) + tid / (64 * NW)));
+  const bool live = id < (long)p.B * p.kv * R;
+  const int pair = live ? (int)(id / R) : 0, r = live ? (int)(id - (long)pair * R) : 0, b = pair / p.kv, hk = pair - b * p.kv;
+  int n, first;
+  tree_parts_of(p, b, lane, n, first);
+  n = __builtin_amdgcn_readfirstlane(n); first = __builtin_amdgcn_readfirstlane(first);
+  const long at = ((long)hk * p.parts + first) * R + r, rows = (long)p.kv * p.parts * R;
   const float *ms = p.part + rows * D + at, *ls = ms + rows;
   float M = -INFINITY;
-#pragma unroll 8
-  for (int s = 0; s < p.nsplit; ++s) M = fmaxf(M, ms[(long)s * R]);
+  for (int s = lane; s < n; s += 64) M = fmaxf(M, ms[(long)s * R]);
+  M = wave_max(M);
   const float M0 = M == -INFINITY ? 0.f : M;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   float L = 0.f;
 #pragma unroll 4
-  for (int s = ng; s < p.nsplit; s += NG) {
+  for (int s = ng; s < n; s += NG) {
     const float a = exp2f(ms[(long)s * R] - M0);
     L = fmaf(ls[(long)s * R], a, L);
     o += *(const f32x4*)(p.part + (at + (long)s * R) * D + 4 * c) * a;
   }
-  if constexpr (NG > 1) {
-    o_s[tid] = o; l_s[tid] = L;
-    __syncthreads();
-    if (ng) return;
-    for (int n = 1; n < NG; ++n) { o += o_s[tid + n * Q]; L += l_s[tid + n * Q]; }
-  }
-  if (!live) return;
-  const int node = r / p.G, hk = (int)(pair % p.kv), b = (int)(pair / p.kv);
+  o_s[tid] = o; l_s[tid] = L;
+  __syncthreads();
+  if (ng || !live) return;
+  const int used = min(NG, n);
+  for (int x = 1; x < used; ++x) { o += o_s[tid + x * Q]; L += l_s[tid + x * Q]; }
+  const int node = r / p.G;
   tree_store4(p, b, node, hk * p.G + r - node * p.G, 4 * c, L > 0.f ? o / L : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
 }

@@ -36,20 +36,21 @@ inline size_t summaries_elements(const bpd_cache& c, int block) {
   return (size_t)c.max_batch * c.n_kv_heads * tiles * 2 * c.head_dim * 64;
 }
 
-struct TreePlan { bool rows; int mt, waves, blocks, nsplit; size_t chosen_at, score_at, bytes; };
-// Kernel (rows: the waves share the keys), row tiles of 16 and waves per workgroup, row blocks, parts that the keys are split into, and what the workspace holds: partial
+struct TreePlan { bool rows; int mt, blocks, nsplit; size_t chosen_at, score_at, bytes; };
+// Kernel (rows: the waves share the keys), row tiles of 16 (per wave), row blocks, parts that the keys are split into, and what the workspace holds: partial
 // results, then (block > 0) bits of the chosen blocks and their bounds.
 inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int block, int cus) {
   TreePlan p{};
   const int R = T * (heads / c.n_kv_heads);
   const bool grouped = cache_grouped(c);
-  p.rows = grouped && R > 64;
-  if (p.rows) { p.mt = 2; p.waves = R > 128 ? 8 : 4; }
-  else { p.mt = grouped ? (R + 15) / 16 : 1; p.waves = 4; }
-  const int per = p.rows ? 16 * p.mt * p.waves : (grouped ? 64 : 16);
+  p.rows = grouped && R > (c.head_dim == 64 ? 64 : 32);
+  p.mt = p.rows ? (R > 64 ? 2 : 1) : (grouped ? (R + 15) / 16 : 1);
+  const int per = p.rows ? 64 * p.mt : (grouped ? 64 : 16);
   p.blocks = (R + per - 1) / per;
   const long pairs = (long)B * c.n_kv_heads * p.blocks, groups = (c.capacity + 31) / 32;
-  long n = (2L * cus + pairs - 1) / pairs, most = groups / 8;
+  // as many parts as give each CU the workgroups that its registers let run at once (fp32 rows: four; 64 rows that share 128-wide keys: three)
+  const int side = !grouped ? 4 : (p.rows && p.mt == 1 ? 3 : 2);
+  long n = ((long)side * cus + pairs - 1) / pairs, most = groups / 8;
   n = n < most ? n : most;
   n = n < 64 ? n : 64;
   p.nsplit = n < 1 ? 1 : (int)n;
