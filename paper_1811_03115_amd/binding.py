@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -64,16 +65,18 @@ EXPORTS = ["bpd_workspace_bytes", "bpd_create", "bpd_destroy", "bpd_load_weights
            "bpd_sparse_attention", "bpd_tree_accept"]
 
 _lib = None
+_torch = None                # torch, once the library is loaded
+_raw_stream = None           # its current stream's handle by device number, where torch has that call
 
 
 def lib() -> C.CDLL:
     """Load libbpd.so.  There is no fallback: without the HIP library nothing runs."""
-    global _lib
+    global _lib, _torch, _raw_stream
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_1811_03115_amd.build` "
                                "(there is no CPU fallback)")
-        import torch  # noqa: F401  (first: the library then uses the HIP runtime that torch brings, not a second one)
+        import torch  # (first: the library then uses the HIP runtime that torch brings, not a second one)
         L = C.CDLL(LIB_PATH)
         vp, i32p = C.c_void_p, C.c_void_p
         L.bpd_workspace_bytes.restype = C.c_size_t
@@ -103,17 +106,18 @@ def lib() -> C.CDLL:
         L.bpd_set_sparse_attention.argtypes = [vp] + [C.c_int] * 4 + [vp, C.c_size_t]
         L.bpd_sparse_buffer_bytes.restype = C.c_size_t
         L.bpd_sparse_buffer_bytes.argtypes = [vp, C.c_int]
-        cp, rp, sz = C.POINTER(bpd_cache), C.POINTER(bpd_rows), C.c_size_t
+        cp, rp, sz = vp, vp, C.c_size_t          # (bpd_cache, bpd_rows, bpd_blocks: by reference, or as packed bytes)
         L.bpd_op_error.restype = C.c_char_p
         L.bpd_op_error.argtypes = []
         for name, args in (("bpd_cache_bytes", [cp]), ("bpd_summaries_bytes", [cp, C.c_int]), ("bpd_attention_workspace_bytes", [cp] + [C.c_int] * 4)):
             getattr(L, name).restype, getattr(L, name).argtypes = sz, args
         L.bpd_cache_store.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, vp]
         L.bpd_tree_attention.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, sz, vp]
-        L.bpd_sparse_attention.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, C.POINTER(bpd_blocks), vp, sz, vp]
+        L.bpd_sparse_attention.argtypes = [cp, rp, rp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, vp, sz, vp]
         L.bpd_tree_accept.argtypes = [vp] * 6 + [C.c_int] * 3 + [vp] * 4 + [cp, vp]
         L.bpd_last_error.restype = C.c_char_p
         L.bpd_last_error.argtypes = [vp]
+        _torch, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _lib = L
     return _lib
 
@@ -173,9 +177,10 @@ def new_cache(max_batch: int, n_kv_heads: int, head_dim: int, capacity: int, dty
 def new_summaries(cache, block: int):
     """Summaries of one layer's blocks for bpd_sparse_attention, zeros."""
     import torch
-    c, k, _ = _cache(cache, 0)
-    tiles = (c.capacity // block + 63) // 64
-    return torch.zeros((c.max_batch, c.n_kv_heads, tiles, 2, c.head_dim // 8, 64, 8), dtype=k.dtype, device=k.device)
+    (_, _, _, _, b, h, d, cap), k, _ = _cache(cache, 0)
+    if block not in (32, 64, 128):
+        raise _bad("block: 32, 64 or 128 rows")
+    return torch.zeros((b, h, (cap // block + 63) // 64, 2, d // 8, 64, 8), dtype=k.dtype, device=k.device)
 
 
 def _op_check(rc: int):
@@ -187,105 +192,117 @@ def _bad(what: str):
     return BpdError(-1, what)
 
 
+# (the wrappers below are most of what a call of a few microseconds costs the host: they look at each tensor once, and pack bpd_cache, bpd_rows and bpd_blocks
+# as bytes, which takes a quarter of what building a ctypes structure does)
+_PACK_CACHE, _PACK_ROWS, _PACK_BLOCKS = struct.Struct("PPiiiiii"), struct.Struct("Pi4xqqqq"), struct.Struct("iiiiPPP")
+_DTYPES = {}                 # torch's dtypes, filled with the first call: this module imports torch late
+_WORKSPACES = {}             # bytes of workspace by the sizes that they depend on
+
+
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BPD_BF16
-    if t.dtype == torch.float32:
-        return BPD_F32
-    raise _bad(f"tensors are bfloat16 or float32, not {t.dtype}")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: BPD_BF16, torch.float32: BPD_F32})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise _bad(f"tensors are bfloat16 or float32, not {t.dtype}")
+    return code
 
 
 def _cache(cache, layer: Optional[int] = None):
-    """bpd_cache of the tensors (k, v); layer: of that one alone.  Returns (struct, k, whether the tensors have a dimension of layers)."""
+    """The tensors (k, v) as a cache; layer: that one alone.  Returns (the fields of bpd_cache, k, whether the tensors have a dimension of layers)."""
     k, v = cache
-    dtype, d = _dtype_of(k), k.shape[-1]
-    grouped = dtype == BPD_BF16 and d in (64, 128)
-    layers = k.dim() - (5 if grouped else 4)
-    if layers not in (0, 1) or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or not k.is_contiguous() or not v.is_contiguous():
+    dtype, shape = _dtype_of(k), k.shape
+    d = shape[-1]
+    grouped = dtype == BPD_BF16 and (d == 64 or d == 128)
+    layers = len(shape) - (5 if grouped else 4)
+    if layers not in (0, 1) or shape != v.shape or k.dtype != v.dtype or k.get_device() != v.get_device() or not k.is_contiguous() or not v.is_contiguous():
         raise _bad("cache: k and v are contiguous tensors of one shape, type and device, as binding.new_cache makes them")
-    n = k.shape[0] if layers else 1
+    n = shape[0] if layers else 1
     kp, vp = k.data_ptr(), v.data_ptr()
     if grouped:
-        b, h, groups, rows, _ = k.shape[layers:]
+        b, h, groups, rows, _ = shape[layers:]
         if rows != 32:
             raise _bad("cache: groups of 32 keys")
         cap = 32 * groups
     else:
-        b, cap, h, _ = k.shape[layers:]
+        b, cap, h, _ = shape[layers:]
     if layer is not None:
         if not 0 <= layer < n:
             raise _bad("cache: no such layer")
-        at = layer * (b * h * cap * d) * k.element_size()
-        kp, vp, n = kp + at, vp + at, 1
-    return bpd_cache(kp, vp, dtype, n, b, h, d, cap), k, layers
+        if layer:
+            at = layer * (b * h * cap * d) * (2 if dtype == BPD_BF16 else 4)
+            kp, vp = kp + at, vp + at
+        n = 1
+    return (kp, vp, dtype, n, b, h, d, cap), k, layers
 
 
-def _same(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise _bad(f"{name} is on {t.device}, the cache on {device}")
-
-
-def _ints(shape, **tensors):
-    """Device int32 arrays of the given shape, contiguous."""
-    import torch
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise _bad(f"{name}: contiguous int32 {list(shape)}")
+def _int(device: int, shape, name: str, t):
+    """Address of an int32 array of the given shape, contiguous, on the device (None: None)."""
+    if t is None:
+        return None
+    if t.dtype != _torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise _bad(f"{name}: contiguous int32 {list(shape)}")
+    if t.get_device() != device:
+        raise _bad(f"{name} is on {t.device}, the cache on another device")
+    return t.data_ptr()
 
 
 def _rows(t, layers: int = 0):
     """bpd_rows of a tensor [layers,] B, T, heads, D whose last dimension is contiguous."""
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise _bad("the last dimension of rows is contiguous")
     s = t.stride()
-    return bpd_rows(t.data_ptr(), _dtype_of(t), s[0] if layers else 0, s[layers], s[layers + 1], s[layers + 2])
+    if s[-1] != 1 and t.shape[-1] > 1:
+        raise _bad("the last dimension of rows is contiguous")
+    return _PACK_ROWS.pack(t.data_ptr(), _dtype_of(t), s[0] if layers else 0, s[layers], s[layers + 1], s[layers + 2])
 
 
-class _on:
-    """The device of a tensor as the current one, and torch's current stream there."""
-
-    def __init__(self, device):
-        import torch
-        if device.type != "cuda":
-            raise _bad("tensors are on a GPU")
-        self.guard = torch.cuda.device(device) if device.index not in (None, torch.cuda.current_device()) else None
-        self.stream = torch.cuda.current_stream(device).cuda_stream
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *a):
-        if self.guard:
-            self.guard.__exit__(*a)
+def _call(device: int, call, *args):
+    """call(*args, stream) on the device, on torch's current stream there."""
+    if device < 0:
+        raise _bad("tensors are on a GPU")
+    stream = _raw_stream(device) if _raw_stream else _torch.cuda.current_stream(device).cuda_stream
+    if device == _torch.cuda.current_device():
+        rc = call(*args, stream)
+    else:
+        with _torch.cuda.device(device):
+            rc = call(*args, stream)
+    if rc:
+        _op_check(rc)
 
 
 def _attention(cache, layer, q, length, parent, scale, out, workspace, block):
-    """What both attentions do with their arguments: (cache, q, out as structs, B, T, heads, scale, workspace, out)."""
-    import torch
+    """What both attentions do with their arguments: (device, the cache's fields, the call's first arguments, workspace, its address and bytes, out)."""
+    lib()
     c, k, _ = _cache(cache, layer)
-    if q.dim() != 4 or q.shape[-1] != c.head_dim:
+    device, shape = k.get_device(), q.shape
+    if len(shape) != 4 or shape[3] != c[6]:
         raise _bad("q: [B, T, heads, head_dim]")
-    b, t, h, d = q.shape
+    b, t, h, d = shape
+    if q.get_device() != device:
+        raise _bad("q and the cache are on different devices")
     if out is None:
-        out = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape:
-        raise _bad("out: the shape of q")
-    _same(k.device, q=q, out=out, length=length, parent=parent, workspace=workspace)
-    _ints((b,), length=length)
-    _ints((b, t), parent=parent)
-    return c, _rows(q), _rows(out), b, t, h, (d ** -0.5 if scale is None else float(scale)), out
-
-
-def _workspace(c, b, t, h, block, workspace, device):
-    import torch
-    need = lib().bpd_attention_workspace_bytes(C.byref(c), b, t, h, block)
+        out = _torch.empty(shape, dtype=q.dtype, device=q.device)
+    elif out.shape != shape or out.get_device() != device:
+        raise _bad("out: the shape and device of q")
+    length_p, parent_p = _int(device, (b,), "length", length), _int(device, (b, t), "parent", parent)
+    if device < 0:
+        raise _bad("tensors are on a GPU")
+    packed = _PACK_CACHE.pack(*c)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    return workspace, (workspace.data_ptr() if workspace is not None else None), (workspace.numel() * workspace.element_size() if workspace is not None else 0)
+        key = (device, c[2:], b, t, h, block)
+        need = _WORKSPACES.get(key)
+        if need is None:
+            with _torch.cuda.device(device):
+                need = lib().bpd_attention_workspace_bytes(packed, b, t, h, block)
+            if len(_WORKSPACES) > 4096:
+                _WORKSPACES.clear()
+            _WORKSPACES[key] = need
+        if need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise _bad("workspace: contiguous, on the cache's device")
+    ws, nbytes = (workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0)
+    return device, c, (packed, _rows(q), _rows(out), length_p, parent_p, b, t, h, d ** -0.5 if scale is None else scale), workspace, ws, nbytes, out
 
 
 class Context:
@@ -486,76 +503,77 @@ class Context:
 
     @staticmethod
     def bpd_cache_bytes(cache) -> int:
-        return lib().bpd_cache_bytes(C.byref(_cache(cache)[0]))
+        return lib().bpd_cache_bytes(_PACK_CACHE.pack(*_cache(cache)[0]))
 
     @staticmethod
     def bpd_summaries_bytes(cache, block: int) -> int:
-        return lib().bpd_summaries_bytes(C.byref(_cache(cache, 0)[0]), block)
+        return lib().bpd_summaries_bytes(_PACK_CACHE.pack(*_cache(cache, 0)[0]), block)
 
     @staticmethod
     def bpd_attention_workspace_bytes(cache, B: int, T: int, n_heads: int, block: int = 0) -> int:
         c, k, _ = _cache(cache, 0)
-        with _on(k.device):
-            return lib().bpd_attention_workspace_bytes(C.byref(c), B, T, n_heads, block)
+        with lib() and _torch.cuda.device(k.device):
+            return lib().bpd_attention_workspace_bytes(_PACK_CACHE.pack(*c), B, T, n_heads, block)
 
     @staticmethod
     def bpd_cache_store(cache, k, v, start, count=None):
         """Rows k, v [B, T, kv heads, head_dim] ([n_layers, B, ..] for a cache with layers) to rows start[b] .. of the cache; count[b] of them (None: T)."""
+        L = lib()
         c, kc, layers = _cache(cache)
-        if k.dim() != 4 + layers or k.shape != v.shape or k.shape[-1] != c.head_dim or k.shape[-2] != c.n_kv_heads or (layers and k.shape[0] != c.n_layers):
+        device, shape = kc.get_device(), k.shape
+        if len(shape) != 4 + layers or shape != v.shape or shape[-1] != c[6] or shape[-2] != c[5] or (layers and shape[0] != c[3]):
             raise _bad("k, v: [B, T, kv heads, head_dim], behind the layers if the cache has any")
-        b, t = k.shape[layers:layers + 2]
-        _same(kc.device, k=k, v=v, start=start, count=count)
-        _ints((b,), start=start, count=count)
-        with _on(kc.device) as stream:
-            _op_check(lib().bpd_cache_store(C.byref(c), C.byref(_rows(k, layers)), C.byref(_rows(v, layers)), start.data_ptr(), None if count is None else count.data_ptr(), b, t, stream))
+        if k.get_device() != device or v.get_device() != device:
+            raise _bad("k, v and the cache are on different devices")
+        b, t = shape[layers], shape[layers + 1]
+        _call(device, L.bpd_cache_store, _PACK_CACHE.pack(*c), _rows(k, layers), _rows(v, layers), _int(device, (b,), "start", start), _int(device, (b,), "count", count), b, t)
 
     @staticmethod
     def bpd_tree_attention(cache, q, length, parent=None, layer: int = 0, scale: Optional[float] = None, out=None, workspace=None):
         """q [B, T, heads, head_dim], length [B], parent [B, T] or None (a chain).  Returns out (of q's dtype, unless given; scale None: head_dim ** -0.5)."""
-        c, qr, outr, b, t, h, scale, out = _attention(cache, layer, q, length, parent, scale, out, workspace, 0)
-        with _on(q.device) as stream:
-            keep, ws, n = _workspace(c, b, t, h, 0, workspace, q.device)
-            _op_check(lib().bpd_tree_attention(C.byref(c), C.byref(qr), C.byref(outr), length.data_ptr(), None if parent is None else parent.data_ptr(), b, t, h, scale, ws, n, stream))
+        device, c, args, keep, ws, n, out = _attention(cache, layer, q, length, parent, scale, out, workspace, 0)
+        _call(device, _lib.bpd_tree_attention, *args, ws, n)
         return out
 
     @staticmethod
     def bpd_sparse_attention(cache, q, length, summaries, block: int, first: int, recent: int, top: int, parent=None, added=None, layer: int = 0,
                              scale: Optional[float] = None, out=None, chosen=None, workspace=None):
         """As bpd_tree_attention, over chosen blocks; summaries: binding.new_summaries(), one per layer.  Returns (out, chosen [B, kv heads, T, words] int32)."""
-        import torch
-        c, qr, outr, b, t, h, scale, out = _attention(cache, layer, q, length, parent, scale, out, workspace, block)
-        _same(q.device, summaries=summaries, added=added, chosen=chosen)
-        _ints((b,), added=added)
-        if lib().bpd_summaries_bytes(C.byref(c), block) != summaries.numel() * summaries.element_size() or not summaries.is_contiguous():
-            raise _bad("block: 32, 64 or 128 rows; summaries: as binding.new_summaries makes them")
-        words = (c.capacity // block + 31) // 32
+        if block not in (32, 64, 128):
+            raise _bad("block: 32, 64 or 128 rows")
+        device, c, args, keep, ws, n, out = _attention(cache, layer, q, length, parent, scale, out, workspace, block)
+        _, _, dtype, _, most, kv, d, cap = c
+        b, t, nb = args[5], args[6], cap // block
+        if (summaries.numel() != most * kv * ((nb + 63) // 64) * 128 * d or _dtype_of(summaries) != dtype or not summaries.is_contiguous() or summaries.get_device() != device):
+            raise _bad("summaries: as binding.new_summaries makes them")
+        shape = (b, kv, t, (nb + 31) // 32)
         if chosen is None:
-            chosen = torch.empty((b, c.n_kv_heads, t, words), dtype=torch.int32, device=q.device)
-        _ints((b, c.n_kv_heads, t, words), chosen=chosen)
-        blocks = bpd_blocks(block, first, recent, top, summaries.data_ptr(), None if added is None else added.data_ptr(), chosen.data_ptr())
-        with _on(q.device) as stream:
-            keep, ws, n = _workspace(c, b, t, h, block, workspace, q.device)
-            _op_check(lib().bpd_sparse_attention(C.byref(c), C.byref(qr), C.byref(outr), length.data_ptr(), None if parent is None else parent.data_ptr(), b, t, h, scale,
-                                                 C.byref(blocks), ws, n, stream))
+            chosen = _torch.empty(shape, dtype=_torch.int32, device=q.device)
+        blocks = _PACK_BLOCKS.pack(block, first, recent, top, summaries.data_ptr(), _int(device, (b,), "added", added) or 0, _int(device, shape, "chosen", chosen))
+        _call(device, _lib.bpd_sparse_attention, *args, blocks, ws, n)
         return out, chosen
 
     @staticmethod
     def bpd_tree_accept(parent, token, expect, best, length, cache=None, room=None, eos_id: int = -1, out=None):
         """parent, token, best [B, T], expect, length, room [B].  Returns (path [B, T], accepted [B], next [B], new_length [B]), or writes them to `out`."""
-        import torch
-        if parent.dim() != 2:
+        L = lib()
+        shape, device = parent.shape, parent.get_device()
+        if len(shape) != 2:
             raise _bad("parent: [B, T]")
-        b, t = parent.shape
-        if out is None:
-            out = (torch.empty_like(parent), torch.empty_like(length), torch.empty_like(length), torch.empty_like(length))
+        b, t = shape
+        one = (b,)
+        if out is None:                            # (a piece of memory for the four of them)
+            path, accepted, following, new_length = _torch.empty(b * (t + 3), dtype=_torch.int32, device=parent.device).split((b * t, b, b, b))
+            path = path.view(shape)
+            out = (path, accepted, following, new_length)
         path, accepted, following, new_length = out
-        _same(parent.device, token=token, expect=expect, best=best, length=length, room=room, path=path, accepted=accepted, next=following, new_length=new_length,
-              cache=None if cache is None else cache[0])
-        _ints((b, t), parent=parent, token=token, best=best, path=path)
-        _ints((b,), expect=expect, length=length, room=room, accepted=accepted, next=following, new_length=new_length)
-        c = None if cache is None else C.byref(_cache(cache)[0])
-        with _on(parent.device) as stream:
-            _op_check(lib().bpd_tree_accept(parent.data_ptr(), token.data_ptr(), expect.data_ptr(), best.data_ptr(), length.data_ptr(), None if room is None else room.data_ptr(), eos_id, b, t,
-                                            path.data_ptr(), accepted.data_ptr(), following.data_ptr(), new_length.data_ptr(), c, stream))
+        c = None
+        if cache is not None:
+            c, k, _ = _cache(cache)
+            if k.get_device() != device:
+                raise _bad("parent and the cache are on different devices")
+            c = _PACK_CACHE.pack(*c)
+        _call(device, L.bpd_tree_accept, _int(device, shape, "parent", parent), _int(device, shape, "token", token), _int(device, one, "expect", expect), _int(device, shape, "best", best),
+              _int(device, one, "length", length), _int(device, one, "room", room), eos_id, b, t, _int(device, shape, "path", path), _int(device, one, "accepted", accepted),
+              _int(device, one, "next", following), _int(device, one, "new_length", new_length), c)
         return out

@@ -134,3 +134,11 @@ def test_wrappers_want_a_gpu():
         binding.Context.bpd_tree_attention(c, torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16), n)
     with pytest.raises(binding.BpdError):
         binding.Context.bpd_cache_store(c, torch.zeros(2, 3, 2, 64), torch.zeros(2, 3, 2, 64), n)
+
+
+def test_packed_structures():
+    """What the wrappers pack as bytes is what the structures hold."""
+    for pack, kind, values in ((binding._PACK_CACHE, binding.bpd_cache, (P, 2 * P, 1, 2, 3, 4, 64, 96)), (binding._PACK_ROWS, binding.bpd_rows, (P, 1, 1 << 40, -5, 7, 64)),
+                               (binding._PACK_BLOCKS, binding.bpd_blocks, (32, 1, 2, 3, P, 2 * P, 3 * P))):
+        got = kind.from_buffer_copy(pack.pack(*values))
+        assert pack.size == C.sizeof(kind) and tuple(getattr(got, f[0]) for f in kind._fields_) == values
