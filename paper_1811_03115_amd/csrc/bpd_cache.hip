@@ -50,7 +50,7 @@ RowsP rows_of(const bpd_rows& r) { return RowsP{r.data, r.dtype == BPD_F32, rows
 template <int D, int MT, int NW, bool SPARSE>
 void attend_few(const TreeP& p, hipStream_t s) {
   const dim3 grid(p.parts, p.kv);
-  if constexpr (MT <= 2) {                       // (queries of fp32 and of many rows take other tiles: attend_groups)
+  if constexpr (MT == 1 || (MT == 2 && D == 64)) {      // (more rows of fp32 queries: attend_groups)
     if (p.q_f32) { hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, true, SPARSE>), grid, dim3(64 * NW), 0, s, p); return; }
   }
   hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, false, SPARSE>), grid, dim3(64 * NW), 0, s, p);
@@ -58,7 +58,7 @@ void attend_few(const TreeP& p, hipStream_t s) {
 template <int D, bool SPARSE>
 void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
   const int R = p.T * p.G;
-  if (plan.rows || (p.q_f32 && R > 32)) {
+  if (plan.rows || (p.q_f32 && R > (D == 64 ? 32 : 16))) {
     if (p.q_f32) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, true, SPARSE>), dim3(p.parts * ((R + 63) / 64), p.kv), dim3(256), 0, s, p);
     else if (plan.mt == 1) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
     else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
@@ -103,7 +103,11 @@ void choose_blocks(const bpd_cache& c, const BoundP& bp, hipStream_t s) {
   else if (D == 16) hipLaunchKernelGGL((block_bounds_kernel<float, 16, false>), grid, dim3(256), 0, s, bp);
   else if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<float, 64, false>), grid, dim3(256), 0, s, bp);
   else hipLaunchKernelGGL((block_bounds_kernel<float, 128, false>), grid, dim3(256), 0, s, bp);
-  if (bp.t.T > 0) hipLaunchKernelGGL(block_pick_kernel, dim3(bp.t.T, bp.t.kv, bp.t.B), dim3(PICK_T), 0, s, bp);
+  if (bp.t.T == 0) return;
+  const dim3 waves((bp.t.T + 3) / 4, bp.t.kv, bp.t.B);
+  if (bp.tiles <= 2) hipLaunchKernelGGL(block_pick_waves_kernel<2>, waves, dim3(256), 0, s, bp);
+  else if (bp.tiles <= 8) hipLaunchKernelGGL(block_pick_waves_kernel<8>, waves, dim3(256), 0, s, bp);
+  else hipLaunchKernelGGL(block_pick_kernel, dim3(bp.t.T, bp.t.kv, bp.t.B), dim3(PICK_T), 0, s, bp);
 }
 // What the blocks of a call are, and where their bounds and bits go
 BoundP bound_args(TreeP& p, const bpd_cache& c, const bpd_blocks& blocks, unsigned* chosen, double* score) {

@@ -112,15 +112,46 @@ struct BoundP {
   double* score;                                 // [b][kv head][node][64 tiles]
   unsigned* chosen;                              // [b][kv head][node][words]
 };
+__device__ __forceinline__ void load8(const bf16_t* k, float (&v)[8]) {
+  const u32x4 w = *(const u32x4*)k;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void load8(const float* k, float (&v)[8]) {
+  const f32x4 x = *(const f32x4*)k, y = *(const f32x4*)(k + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { v[j] = x[j]; v[4 + j] = y[j]; }
+}
+// A wave's dimensions of the bounds of 64 blocks (one per lane) for NN nodes
+template <typename S, int D, int NN>
+__device__ __forceinline__ void bound_sums(const S* sum, const double (*q_s)[2][D], double (*sum_s)[8][64], int wave, int lane) {
+  constexpr int C8 = D / 8;                      // (16 dimensions: two pieces of eight, for two of the waves)
+  double acc[NN];
+#pragma unroll
+  for (int n = 0; n < NN; ++n) acc[n] = 0;
+#pragma unroll 2
+  for (int x = wave; x < C8; x += 4) {
+    float lo[8], hi[8];
+    load8(sum + ((size_t)x * 64 + lane) * 8, lo);
+    load8(sum + ((size_t)(C8 + x) * 64 + lane) * 8, hi);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const double l = (double)lo[j], h = (double)hi[j];
+#pragma unroll
+      for (int n = 0; n < NN; ++n) { acc[n] = fma(q_s[n][0][8 * x + j], h, acc[n]); acc[n] = fma(q_s[n][1][8 * x + j], l, acc[n]); }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NN; ++n) sum_s[wave][n][lane] = acc[n];
+}
 // Upper bound of a group's scores in a block, summed over its G heads:  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
 // the heads are added first and cost nothing.  In 64 bits: products of bf16 numbers and their sums are then as good as exact, and which blocks are chosen does not
 // depend on an order of summation.  (2 D multiply-adds per block and node, an eighth of those of 32 keys with G = 2: 1 .. 2 us.)
 // One tile of 64 blocks of one (sequence, key head) per workgroup: a block per lane, the waves share the dimensions and meet in LDS.
 template <typename S, int D, bool GROUPED>
 __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
-  constexpr int RC = 8, PART = D / 4;            // nodes at a time; dimensions per wave
-  constexpr int BYTES = RC * 2 * D * 8 > 4096 * (int)sizeof(S) ? RC * 2 * D * 8 : 4096 * (int)sizeof(S);
-  __shared__ __attribute__((aligned(16))) unsigned char buf_s[BYTES];
+  constexpr int RC = 8;                          // nodes at a time
+  __shared__ __attribute__((aligned(16))) unsigned char buf_s[RC * 2 * D * 8];
   double (*q_s)[2][D] = (double (*)[2][D])buf_s;                        // sums over the group of the positive and of the negative parts
   __shared__ double sum_s[4][RC][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), tile = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
@@ -134,44 +165,48 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
   int from = p.added_all < 0 ? 0 : max(0, len - p.added_all) / p.block;
   if (p.added) { const int n = p.added[b]; from = n < 0 ? done : (n >= len ? 0 : (len - n) / p.block); }
   const int f0 = max(from, blk0), f1 = min(done, blk0 + 64);
-  for (int blk = f0; blk < f1; ++blk) {
-    // (a thread has eight, or one, dimensions of some of the rows: the threads meet in LDS)
-    S* lo_s = (S*)buf_s;                         // [256 / (D / 8)][D] smallest, then as many largest
-    constexpr int W = D / 8, PER = 256 / W;
-    const int w = tid % W, rr = tid / W;
+  constexpr int W = D / 8, PER = 256 / W;
+  float (*part_s)[2][D] = (float (*)[2][D])buf_s;                       // [wave][smallest, largest]
+  for (int blk = f0; blk < f1; ++blk) {          // a thread has eight dimensions of every PER-th row; lanes of the same dimensions meet by moves, waves in LDS
+    const int w = tid % W;
     float mn[8], mx[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) { mn[j] = INFINITY; mx[j] = -INFINITY; }
-    for (int r = rr; r < p.block; r += PER) {
+    for (int r = tid / W; r < p.block; r += PER) {
       const int key = blk * p.block + r;
       const S* k;
       if constexpr (GROUPED) k = (const S*)p.t.K + (own * p.t.kv + hk) * p.t.cap * D + k_at<D>(key, 8 * w);
       else k = (const S*)p.t.K + (own * p.t.cap + key) * p.t.kv * D + (size_t)hk * D + 8 * w;
+      float v[8];
+      load8(k, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { const float v = to_f<S>(k[j]); mn[j] = fminf(mn[j], v); mx[j] = fmaxf(mx[j], v); }
+      for (int j = 0; j < 8; ++j) { mn[j] = fminf(mn[j], v[j]); mx[j] = fmaxf(mx[j], v[j]); }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { lo_s[rr * D + 8 * w + j] = from_f<S>(mn[j]); lo_s[(PER + rr) * D + 8 * w + j] = from_f<S>(mx[j]); }
-    __syncthreads();
-    if (tid < 2 * W) {
-      const int big = tid / W, c = tid % W * 8;
+    for (int x = W; x < 64; x <<= 1)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float v = to_f<S>(lo_s[big * PER * D + c + j]);
-        for (int r = 1; r < PER && r < p.block; ++r) { const float u = to_f<S>(lo_s[(big * PER + r) * D + c + j]); v = big ? fmaxf(v, u) : fminf(v, u); }
-        sum[((size_t)(big * W + c / 8) * 64 + blk - blk0) * 8 + j] = from_f<S>(v);
-      }
+      for (int j = 0; j < 8; ++j) { mn[j] = fminf(mn[j], __shfl_xor(mn[j], x, 64)); mx[j] = fmaxf(mx[j], __shfl_xor(mx[j], x, 64)); }
+    if (lane < W) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { part_s[wave][0][8 * w + j] = mn[j]; part_s[wave][1][8 * w + j] = mx[j]; }
     }
     __syncthreads();
+    if (tid < 2 * D) {
+      const int big = tid / D, c = tid - big * D;
+      float v = part_s[0][big][c];
+#pragma unroll
+      for (int x = 1; x < 4; ++x) { const float u = part_s[x][big][c]; v = big ? fmaxf(v, u) : fminf(v, u); }
+      sum[((size_t)(big * W + c / 8) * 64 + blk - blk0) * 8 + c % 8] = from_f<S>(v);
+    }
+    __syncthreads();                             // (and what has been written is there for all of the workgroup)
   }
-  if (f1 > f0) { __threadfence_block(); __syncthreads(); }
   const TreeP& t = p.t;
   for (int n0 = 0; n0 < t.T; n0 += RC) {
     const int nn = min(RC, t.T - n0);
-    for (int x = tid; x < nn * D; x += 256) {
+    for (int x = tid; x < RC * D; x += 256) {
       const int n = x / D, c = x - n * D;
       double pos = 0, neg = 0;
-      for (int g = 0; g < t.G; ++g) {
+      for (int g = 0; n < nn && g < t.G; ++g) {
         const long at = (long)b * t.q_seq + (long)(n0 + n) * t.q_row + (long)(hk * t.G + g) * t.q_head + c;
         const float v = t.q_f32 ? ((const float*)t.q)[at] : bf2f(((const bf16_t*)t.q)[at]);
         pos += v > 0.f ? (double)v : 0.0;
@@ -181,23 +216,9 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
       q_s[n][0][c] = pos; q_s[n][1][c] = neg;
     }
     __syncthreads();
-    double acc[RC];
-#pragma unroll
-    for (int n = 0; n < RC; ++n) acc[n] = 0;
-    for (int c = wave * PART; c < (wave + 1) * PART; c += 4) {
-      float mn[4], mx[4];
-      const S* a = sum + ((size_t)(c / 8) * 64 + lane) * 8 + (c & 7);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { mn[j] = to_f<S>(a[j]); mx[j] = to_f<S>(a[D * 64 + j]); }
-#pragma unroll
-      for (int n = 0; n < RC; ++n) {
-        if (n >= nn) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { acc[n] = fma(q_s[n][0][c + j], (double)mx[j], acc[n]); acc[n] = fma(q_s[n][1][c + j], (double)mn[j], acc[n]); }
-      }
-    }
-#pragma unroll
-    for (int n = 0; n < RC; ++n) if (n < nn) sum_s[wave][n][lane] = acc[n];
+    if (nn == 1) bound_sums<S, D, 1>(sum, q_s, sum_s, wave, lane);
+    else if (nn <= 4) bound_sums<S, D, 4>(sum, q_s, sum_s, wave, lane);
+    else bound_sums<S, D, 8>(sum, q_s, sum_s, wave, lane);
     __syncthreads();
     for (int x = tid; x < nn * 64; x += 256) {
       const int n = x >> 6, l = x & 63;
@@ -207,7 +228,75 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
   }
 }
 
-// The blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the lower block; a bound that
+// Order-preserving key of a bound: a larger one has a larger key, one that is no number the smallest
+__device__ __forceinline__ unsigned long long bound_key(double score) {
+  const double s = score + 0.0;                  // (no negative zero)
+  const unsigned long long u = (unsigned long long)__double_as_longlong(s);
+  return s != s ? 1ull : (u >> 63 ? ~u : u | 1ull << 63);
+}
+// Up to 64 N blocks: a wave per (node, key head, sequence), N bounds a lane, all in registers: the largest threshold that `take` keys reach is found bit by bit from the first bit
+// in which they differ, each bit a count of ballots, until exactly as many reach it.  No LDS and no barriers.  (94 blocks: 11.3 us with the digits below)
+template <int N>
+__global__ __launch_bounds__(256) void block_pick_waves_kernel(BoundP p) {
+  const TreeP& t = p.t;
+  const int lane = threadIdx.x & 63, n = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), hk = blockIdx.y, b = blockIdx.z;
+  if (n >= t.T) return;
+  const size_t row = ((size_t)b * t.kv + hk) * t.T + n;
+  const double* score = p.score + row * p.tiles * 64;
+  double s[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) s[j] = j < p.tiles ? score[64 * j + lane] : 0.0;
+  int len, there;
+  tree_extent(t, b, len, there);
+  mask64 anc; bool ok;
+  tree_ancestors(t, b, there, lane, anc, ok);
+  const bool there_n = __ballot(ok) >> n & 1;
+  const int done = len / p.block, lo = min(p.first, done), hi = max(lo, done - p.recent), cand = hi - lo, take = min(p.top, cand);
+  unsigned long long key[N], a = ~0ull, o = 0ull;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int blk = 64 * j + lane;
+    const bool in = blk >= lo && blk < hi;
+    key[j] = in ? bound_key(s[j]) : 0ull;        // (0: no candidate's)
+    if (in) { a &= key[j]; o |= key[j]; }
+  }
+  // chosen: keys of at least thr, and the lowest `ties` blocks whose key is `tie`
+  unsigned long long thr = 1, tie = 0;
+  int ties = 0;
+  if (take == 0) thr = ~0ull;                    // (no bound has that key: it would be a NaN)
+  else if (take < cand) {
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) { a &= __shfl_xor(a, x, 64); o |= __shfl_xor(o, x, 64); }
+    const unsigned long long differ = a ^ o;
+    int bit = differ ? 63 - __clzll((long long)differ) : -1;
+    thr = bit < 0 ? a : (bit == 63 ? 0ull : a >> (bit + 1) << (bit + 1));
+    int above = 0;                               // keys over the final threshold's bits so far
+    bool exact = false;
+    for (; bit >= 0 && !exact; --bit) {
+      const unsigned long long c = thr | 1ull << bit;
+      int cnt = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) cnt += __popcll(__ballot(key[j] >= c));
+      if (cnt >= take) { thr = c; exact = cnt == take; } else above = cnt;
+    }
+    if (!exact) { tie = thr; ties = take - above; thr = thr + 1; }       // more keys equal the threshold than are wanted
+  }
+  unsigned* out = p.chosen + row * t.words;
+  int before = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int blk = 64 * j + lane;
+    const bool in = blk >= lo && blk < hi, same = in && ties && key[j] == tie;
+    const mask64 m = __ballot(same);
+    const bool mine = same && before + __popcll(m & ((1ull << lane) - 1)) < ties;
+    before += __popcll(m);
+    const bool pick = there_n && blk < done && (!in || mine || key[j] >= thr);
+    const mask64 bits = __ballot(pick);
+    if (lane < 2 && 2 * j + lane < t.words) out[2 * j + lane] = (unsigned)(bits >> (32 * lane));
+  }
+}
+
+// More blocks: a workgroup for the blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the lower block; a bound that
 // is no number comes last.  Order-preserving 64-bit keys; a digit of eight bits at a time from the first bit in which they differ (most keys share sign and exponent,
 // and a histogram of those would be one counter), until the digit that the last chosen one is in holds no more than are wanted.
 constexpr int PICK_T = 512, PICK_N = TREE_BLOCKS_MAX / PICK_T;
@@ -244,9 +333,7 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
       const int blk = j * PICK_T + tid;
       key[j] = 0;
       if (blk >= lo && blk < hi) {
-        const double s = score[blk] + 0.0;       // (no negative zero)
-        const unsigned long long u = (unsigned long long)__double_as_longlong(s);
-        key[j] = s != s ? 1ull : (u >> 63 ? ~u : u | 1ull << 63);
+        key[j] = bound_key(score[blk]);
         a &= key[j]; o |= key[j];
       }
     }
