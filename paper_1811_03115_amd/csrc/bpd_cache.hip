@@ -94,7 +94,7 @@ void attend(const bpd_cache& c, const TreeP& args, const TreePlan& plan, hipStre
 
 // Bounds of the blocks, with fresh summaries (no nodes: those alone), and the blocks that each node sees
 void choose_blocks(const bpd_cache& c, const BoundP& bp, hipStream_t s) {
-  const dim3 grid(bp.tiles, bp.t.kv, bp.t.B);
+  const dim3 grid(bp.tiles * (bp.t.T > 16 ? (bp.t.T + 15) / 16 : 1), bp.t.kv, bp.t.B);
   const int D = c.head_dim;
   if (cache_grouped(c)) {
     if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<bf16_t, 64, true>), grid, dim3(256), 0, s, bp);

@@ -112,75 +112,88 @@ struct BoundP {
   double* score;                                 // [b][kv head][node][64 tiles]
   unsigned* chosen;                              // [b][kv head][node][words]
 };
-__device__ __forceinline__ void load8(const bf16_t* k, float (&v)[8]) {
-  const u32x4 w = *(const u32x4*)k;
+// Eight of a cache's elements as they come
+template <typename S> struct Eight;
+template <> struct Eight<bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t* k) { w = *(const u32x4*)k; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
-}
-__device__ __forceinline__ void load8(const float* k, float (&v)[8]) {
-  const f32x4 x = *(const f32x4*)k, y = *(const f32x4*)(k + 4);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) { v[j] = x[j]; v[4 + j] = y[j]; }
-}
-// A wave's dimensions of the bounds of 64 blocks (one per lane) for NN nodes
-template <typename S, int D, int NN>
-__device__ __forceinline__ void bound_sums(const S* sum, const double (*q_s)[2][D], double (*sum_s)[8][64], int wave, int lane) {
-  constexpr int C8 = D / 8;                      // (16 dimensions: two pieces of eight, for two of the waves)
-  double acc[NN];
-#pragma unroll
-  for (int n = 0; n < NN; ++n) acc[n] = 0;
-#pragma unroll 2
-  for (int x = wave; x < C8; x += 4) {
-    float lo[8], hi[8];
-    load8(sum + ((size_t)x * 64 + lane) * 8, lo);
-    load8(sum + ((size_t)(C8 + x) * 64 + lane) * 8, hi);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const double l = (double)lo[j], h = (double)hi[j];
-#pragma unroll
-      for (int n = 0; n < NN; ++n) { acc[n] = fma(q_s[n][0][8 * x + j], h, acc[n]); acc[n] = fma(q_s[n][1][8 * x + j], l, acc[n]); }
-    }
+    for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
   }
+};
+template <> struct Eight<float> {
+  f32x4 x, y;
+  __device__ __forceinline__ void load(const float* k) { x = *(const f32x4*)k; y = *(const f32x4*)(k + 4); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-  for (int n = 0; n < NN; ++n) sum_s[wave][n][lane] = acc[n];
-}
+    for (int j = 0; j < 4; ++j) { v[j] = x[j]; v[4 + j] = y[j]; }
+  }
+};
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 // Upper bound of a group's scores in a block, summed over its G heads:  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
-// the heads are added first and cost nothing.  In 64 bits: products of bf16 numbers and their sums are then as good as exact, and which blocks are chosen does not
-// depend on an order of summation.  (2 D multiply-adds per block and node, an eighth of those of 32 keys with G = 2: 1 .. 2 us.)
-// One tile of 64 blocks of one (sequence, key head) per workgroup: a block per lane, the waves share the dimensions and meet in LDS.
+// the heads are added first and cost nothing, and what is left is a product of 16 nodes with 64 blocks over 2 D.  In 64 bits, on v_mfma_f64_16x16x4_f64: products of bf16 numbers and
+// their sums are then as good as exact, and which blocks are chosen does not depend on an order of summation.  (On the vector units the nodes' sums, the same for all lanes, come out
+// of LDS once per block and wave, which bounds it: 7 nodes, 1000 blocks of 128 dimensions in 32 pairs 13.6 us.)
+// One tile of 64 blocks of one (sequence, key head), and 16 nodes, per workgroup: a wave has 16 blocks, and of 32 dimensions at a time lane 16 q + c eight of block c.
+// Blocks that the last rows have touched are summarised first, by each of a tile's workgroups (the same values; one block in most calls).
 template <typename S, int D, bool GROUPED>
 __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
-  constexpr int RC = 8;                          // nodes at a time
-  __shared__ __attribute__((aligned(16))) unsigned char buf_s[RC * 2 * D * 8];
-  double (*q_s)[2][D] = (double (*)[2][D])buf_s;                        // sums over the group of the positive and of the negative parts
-  __shared__ double sum_s[4][RC][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), tile = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  constexpr int C8 = D / 8, W = C8, PER = 256 / W;
+  __shared__ double q_s[2 * C8][8][17];          // [eight dimensions: negative parts, then positive][dimension][node]
+  __shared__ float part_s[4][2][D];              // [wave][smallest, largest]
+  const TreeP& t = p.t;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hk = blockIdx.y, b = blockIdx.z;
+  const int tile = blockIdx.x % p.tiles, n0 = blockIdx.x / p.tiles * 16, nn = min(16, t.T - n0);
+  // (nothing of this waits for the length: summaries, as far as they stay, and queries)
+  const size_t own = tree_cache(t, b);
+  S* sum = (S*)p.summaries + ((own * t.kv + hk) * p.tiles + tile) * (2 * D * 64);
+  const int c = lane & 15, q = lane >> 4;
+  Eight<S> v[C8 / 2];
+  auto load = [&]() {
+#pragma unroll
+    for (int x = 0; x < C8 / 2; ++x) v[x].load(sum + ((size_t)(4 * x + q) * 64 + 16 * wave + c) * 8);
+  };
+  if (nn > 0) load();
+  for (int x = tid; x < 16 * C8; x += 256) {
+    const int n = x & 15, c8 = x >> 4;
+    double pos[8] = {}, neg[8] = {};
+    if (n < nn) {
+#pragma unroll 4
+      for (int g = 0; g < t.G; ++g) {
+        float v[8];
+        tree_q8(t, b, n0 + n, hk * t.G + g, 8 * c8, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { pos[j] += (double)(v[j] < 0.f ? 0.f : v[j]); neg[j] += (double)(v[j] > 0.f ? 0.f : v[j]); }      // (one that is no number goes to both)
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { q_s[c8][j][n] = neg[j]; q_s[C8 + c8][j][n] = pos[j]; }
+  }
   int len, there;
-  tree_extent(p.t, b, len, there);
+  tree_extent(t, b, len, there);
   const int done = len / p.block, blk0 = 64 * tile;
   if (blk0 >= done) return;
-  const size_t own = tree_cache(p.t, b);
-  S* sum = (S*)p.summaries + ((own * p.t.kv + hk) * p.tiles + tile) * (2 * D * 64);
-  // blocks that the last rows have touched
   int from = p.added_all < 0 ? 0 : max(0, len - p.added_all) / p.block;
   if (p.added) { const int n = p.added[b]; from = n < 0 ? done : (n >= len ? 0 : (len - n) / p.block); }
   const int f0 = max(from, blk0), f1 = min(done, blk0 + 64);
-  constexpr int W = D / 8, PER = 256 / W;
-  float (*part_s)[2][D] = (float (*)[2][D])buf_s;                       // [wave][smallest, largest]
   for (int blk = f0; blk < f1; ++blk) {          // a thread has eight dimensions of every PER-th row; lanes of the same dimensions meet by moves, waves in LDS
     const int w = tid % W;
     float mn[8], mx[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) { mn[j] = INFINITY; mx[j] = -INFINITY; }
+#pragma unroll 4
     for (int r = tid / W; r < p.block; r += PER) {
       const int key = blk * p.block + r;
       const S* k;
-      if constexpr (GROUPED) k = (const S*)p.t.K + (own * p.t.kv + hk) * p.t.cap * D + k_at<D>(key, 8 * w);
-      else k = (const S*)p.t.K + (own * p.t.cap + key) * p.t.kv * D + (size_t)hk * D + 8 * w;
-      float v[8];
-      load8(k, v);
+      if constexpr (GROUPED) k = (const S*)t.K + (own * t.kv + hk) * t.cap * D + k_at<D>(key, 8 * w);
+      else k = (const S*)t.K + (own * t.cap + key) * t.kv * D + (size_t)hk * D + 8 * w;
+      Eight<S> e;
+      float f[8];
+      e.load(k);
+      e.get(f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { mn[j] = fminf(mn[j], v[j]); mx[j] = fmaxf(mx[j], v[j]); }
+      for (int j = 0; j < 8; ++j) { mn[j] = fminf(mn[j], f[j]); mx[j] = fmaxf(mx[j], f[j]); }
     }
 #pragma unroll
     for (int x = W; x < 64; x <<= 1)
@@ -200,31 +213,25 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
     }
     __syncthreads();                             // (and what has been written is there for all of the workgroup)
   }
-  const TreeP& t = p.t;
-  for (int n0 = 0; n0 < t.T; n0 += RC) {
-    const int nn = min(RC, t.T - n0);
-    for (int x = tid; x < RC * D; x += 256) {
-      const int n = x / D, c = x - n * D;
-      double pos = 0, neg = 0;
-      for (int g = 0; n < nn && g < t.G; ++g) {
-        const long at = (long)b * t.q_seq + (long)(n0 + n) * t.q_row + (long)(hk * t.G + g) * t.q_head + c;
-        const float v = t.q_f32 ? ((const float*)t.q)[at] : bf2f(((const bf16_t*)t.q)[at]);
-        pos += v > 0.f ? (double)v : 0.0;
-        neg += v < 0.f ? (double)v : 0.0;
-        if (v != v) pos = neg = (double)v;
-      }
-      q_s[n][0][c] = pos; q_s[n][1][c] = neg;
+  if (nn <= 0) return;                           // (summaries alone)
+  if (f1 > f0) load();
+  __syncthreads();
+  f64x4 acc = f64x4{0, 0, 0, 0}, odd = acc;      // (two chains)
+#pragma unroll
+  for (int x = 0; x < C8 / 2; ++x) {
+    float f[8];
+    v[x].get(f);
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q_s[4 * x + q][j][c], (double)f[j], acc, 0, 0, 0);
+      odd = __builtin_amdgcn_mfma_f64_16x16x4f64(q_s[4 * x + q][j + 1][c], (double)f[j + 1], odd, 0, 0, 0);
     }
-    __syncthreads();
-    if (nn == 1) bound_sums<S, D, 1>(sum, q_s, sum_s, wave, lane);
-    else if (nn <= 4) bound_sums<S, D, 4>(sum, q_s, sum_s, wave, lane);
-    else bound_sums<S, D, 8>(sum, q_s, sum_s, wave, lane);
-    __syncthreads();
-    for (int x = tid; x < nn * 64; x += 256) {
-      const int n = x >> 6, l = x & 63;
-      p.score[((((size_t)b * t.kv + hk) * t.T + n0 + n) * p.tiles + tile) * 64 + l] = (sum_s[0][n][l] + sum_s[1][n][l]) + (sum_s[2][n][l] + sum_s[3][n][l]);
-    }
-    __syncthreads();
+  }
+  acc += odd;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                  // node 4 i + q, block c of the wave's
+    const int n = 4 * i + q;
+    if (n < nn) p.score[((((size_t)b * t.kv + hk) * t.T + n0 + n) * p.tiles + tile) * 64 + 16 * wave + c] = acc[i];
   }
 }
 
