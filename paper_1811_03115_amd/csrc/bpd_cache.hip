@@ -5,6 +5,7 @@
 #include "bpd_cache_launch.h"
 #include "bpd_cache_logic.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <string>
@@ -75,9 +76,14 @@ void join(const TreeP& p, hipStream_t s) {
   else hipLaunchKernelGGL((tree_join_kernel<D, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, p);
 }
 template <bool SPARSE>
-void attend(const bpd_cache& c, const TreeP& args, const TreePlan& plan, hipStream_t s) {
+void attend(const bpd_cache& c, const TreeP& args, TreePlan plan, hipStream_t s, const BoundP* blocks = nullptr) {
   const int D = c.head_dim;
   TreeP p = args;
+  if (SPARSE) {                                  // at most so many groups are seen: fewer parts than the workspace has room for
+    const BoundP& bp = *blocks;
+    const long most = std::min((long)(c.capacity + 31) / 32, (long)std::min<long>(p.T, 1 + p.T / 4) * ((long)bp.first + bp.recent + bp.top) * p.bg + p.bg + 4);
+    plan.nsplit = std::min(plan.nsplit, split_of(plan, (long)p.B * p.kv * plan.blocks, most, cache_grouped(c), compute_units()));
+  }
   // (by length: a lane knows one sequence's; its sums cost some 1 us, which short caches do not have; chosen blocks are about as many in every sequence)
   p.nsplit = plan.nsplit; p.parts = p.B * plan.nsplit; p.by_length = !SPARSE && plan.nsplit > 1 && p.B > 1 && p.B <= 64 && c.capacity >= 4096;
   if (cache_grouped(c)) {
@@ -163,7 +169,7 @@ void launch_block_attention(const BlockAttention& a, hipStream_t stream) {
   BoundP bp = bound_args(p, c, *a.blocks, (unsigned*)((char*)a.scratch + plan.chosen_at), (double*)((char*)a.scratch + plan.score_at));
   bp.added_all = a.added;
   choose_blocks(c, bp, stream);
-  attend<true>(c, p, plan, stream);
+  attend<true>(c, p, plan, stream, &bp);
 }
 void launch_summaries(const bpd_cache& c, const int* length, int B, int block, void* summaries, hipStream_t stream) {
   if (c.capacity < block) return;
@@ -256,8 +262,9 @@ int bpd_sparse_attention(const bpd_cache* c, const bpd_rows* q, const bpd_rows* 
     return launched("bpd_sparse_attention");
   }
   unsigned* chosen = blocks->chosen ? blocks->chosen : (unsigned*)((char*)workspace + plan.chosen_at);
-  choose_blocks(*c, bound_args(p, *c, *blocks, chosen, (double*)((char*)workspace + plan.score_at)), s);
-  attend<true>(*c, p, plan, s);
+  const BoundP bp = bound_args(p, *c, *blocks, chosen, (double*)((char*)workspace + plan.score_at));
+  choose_blocks(*c, bp, s);
+  attend<true>(*c, p, plan, s, &bp);
   return launched("bpd_sparse_attention");
 }
 

@@ -161,12 +161,23 @@ struct TreeItems {
   }
 };
 constexpr int TREE_BLOCKS_MAX = 4096;            // blocks of rows that can be chosen from
-// List of the blocks that any node n0 .. n1 - 1 has chosen, in order; bits: [TREE_BLOCKS_MAX / 32] words of scratch.  All threads; blocks of threads >= words.
-__device__ __forceinline__ int tree_list(const unsigned* chosen, int words, int n0, int n1, int done, unsigned short* list, int* sums) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// List of the blocks that any node n0 .. n1 - 1 has chosen, in order, by all threads (at least as many as there are words).  The nodes' words are dealt to the threads: one trip to
+// memory for up to 256 of them.  (A thread per word that walks the nodes: 0.5 us each.)
+__device__ __forceinline__ int tree_list(const unsigned* chosen, int words, int n0, int n1, int done, unsigned short* list, int* sums, unsigned* bits_s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, parts = (int)blockDim.x / words;
+  if (tid < words) bits_s[tid] = 0;
+  __syncthreads();
+  if (tid < parts * words) {
+    const int part = tid / words, w = tid - part * words;
+    unsigned any = 0;
+#pragma unroll 4
+    for (int n = n0 + part; n < n1; n += parts) any |= chosen[(long)n * words + w];
+    if (any) atomicOr(&bits_s[w], any);
+  }
+  __syncthreads();
   unsigned bits = 0;
   if (tid < words) {
-    for (int n = n0; n < n1; ++n) bits |= chosen[(long)n * words + tid];
+    bits = bits_s[tid];
     const int left = done - 32 * tid;            // (bits past the last complete block: none are set)
     if (left < 32) bits = left <= 0 ? 0u : bits & ((1u << left) - 1u);
   }
@@ -319,6 +330,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
   __shared__ float m_s[NW][MT * 16], l_s[NW][MT * 16];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[NW];
+  __shared__ unsigned bits_s[SPARSE ? TREE_BLOCKS_MAX / 32 : 1];
   static_assert(!Q_LDS || MT * KS <= SLOTS * VT, "queries fit where the results meet");
   u32x4 (*q_s)[KS][64] = (u32x4 (*)[KS][64])&o_s[0][0][0];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
@@ -366,7 +378,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
     picks = p.chosen + pair * p.T * p.words;
     const int done = len / (32 * p.bg);
     it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
-    it.listed = tree_list(picks, p.words, 0, p.T, done, list_s, sums_s) * p.bg;
+    it.listed = tree_list(picks, p.words, 0, p.T, done, list_s, sums_s, bits_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
   if constexpr (Q_LDS) __syncthreads();
@@ -463,6 +475,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
   __shared__ __attribute__((aligned(16))) u32x4 kv_s[2][2 * PIECES];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[NW];
+  __shared__ unsigned bits_s[SPARSE ? TREE_BLOCKS_MAX / 32 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
   const int at_part = blockIdx.x % p.parts, rb = blockIdx.x / p.parts, hk = blockIdx.y, R = p.T * p.G, r0 = (rb * NW + wave) * 16 * MT;
   const TreePart part = tree_part(p, at_part, lane);
@@ -491,7 +504,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
     picks = p.chosen + pair * p.T * p.words;
     const int done = len / (32 * p.bg), w0 = rb * NW * 16 * MT, w1 = min(R, w0 + NW * 16 * MT);
     it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
-    it.listed = tree_list(picks, p.words, w0 / p.G, (w1 + p.G - 1) / p.G, done, list_s, sums_s) * p.bg;
+    it.listed = tree_list(picks, p.words, w0 / p.G, (w1 + p.G - 1) / p.G, done, list_s, sums_s, bits_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
   const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);
@@ -512,19 +525,24 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
 #pragma unroll
     for (int x = 0; x < PER; ++x) kv_s[buf][tid + x * 64 * NW] = kvn[x];
   };
+  unsigned word[SPARSE ? MT : 1];                // has the row chosen the item's block?
+  auto load_words = [&](int ii, int gg) {
+    if constexpr (SPARSE) {
+      const int blk = gg / p.bg;
+#pragma unroll
+      for (int t = 0; t < MT; ++t) word[t] = ii < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
+    }
+  };
   int g = 0;
-  if (i0 < i1) { g = __builtin_amdgcn_readfirstlane(it.group(i0)); ask(g); put(0); }
+  if (i0 < i1) { g = __builtin_amdgcn_readfirstlane(it.group(i0)); load_words(i0, g); ask(g); put(0); }
   __syncthreads();
   for (int i = i0; i < i1; ++i) {
     const int buf = (i - i0) & 1;
     const int gn = i + 1 < i1 ? __builtin_amdgcn_readfirstlane(it.group(i + 1)) : g;
-    unsigned word[SPARSE ? MT : 1];
-    if constexpr (SPARSE) {
-      const int blk = g / p.bg;
+    unsigned now[SPARSE ? MT : 1];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) word[t] = i < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
-    }
-    if (i + 1 < i1) ask(gn);
+    for (int t = 0; t < (SPARSE ? MT : 0); ++t) now[t] = word[t];
+    if (i + 1 < i1) { load_words(i + 1, gn); ask(gn); }
     u32x4 kf[2 * KS], vf[VT];
 #pragma unroll
     for (int x = 0; x < 2 * KS; ++x) kf[x] = kv_s[buf][x * 64 + lane];
@@ -532,7 +550,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
     for (int x = 0; x < VT; ++x) vf[x] = kv_s[buf][PIECES + x * 64 + lane];
     bool vis[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && word[t]; }
+    for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && now[t]; }
     const int at = 32 * g + 8 * lq - len;
     const bool edge = 32 * g + 32 > len;
     if (edge) tree_blank<VT>(vf, at, present);
@@ -559,6 +577,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   __shared__ float m_s[4][16], l_s[4][16];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[4];
+  __shared__ unsigned bits_s[SPARSE ? TREE_BLOCKS_MAX / 32 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
   const int at_part = blockIdx.x % p.parts, rb = blockIdx.x / p.parts, hk = blockIdx.y, R = p.T * p.G, r0 = rb * 16;
   const TreePart part = tree_part(p, at_part, lane);
@@ -588,7 +607,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
     picks = p.chosen + ((long)b * p.kv + hk) * p.T * p.words;
     const int done = len / (32 * p.bg), n0 = r0 / p.G, n1 = min(p.T, (min(R, r0 + 16) + p.G - 1) / p.G);
     it.list = list_s; it.bg = p.bg; it.tail0 = done * p.bg;
-    it.listed = tree_list(picks, p.words, n0, n1, done, list_s, sums_s) * p.bg;
+    it.listed = tree_list(picks, p.words, n0, n1, done, list_s, sums_s, bits_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
   const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);

@@ -37,6 +37,19 @@ inline size_t summaries_elements(const bpd_cache& c, int block) {
 }
 
 struct TreePlan { bool rows; int mt, blocks, nsplit; size_t chosen_at, score_at, bytes; };
+// Parts that `groups` of 32 keys are split into, for as many (sequence, key head, row block)s as there are: the fewest rounds of as many workgroups as the chip has room for (a CU's
+// registers: four of fp32 rows, three of 64 rows that share 128-wide keys, otherwise two) times what a workgroup takes, in units of an item: its items (one in four where the
+// waves split them) and five for its beginning and end; four more for joining parts.  (52 x 4 row blocks over 46 groups: three parts, 624 workgroups, 74 us; two 51.
+// 64 pairs, 95 groups: one part 29 us, four 21, eight 17.)
+inline int split_of(const TreePlan& p, long pairs, long groups, bool grouped, int cus) {
+  const long room = (long)(!grouped ? 4 : (p.rows && p.mt == 1 ? 3 : 2)) * cus, step = p.rows ? 1 : 4;
+  long best = 1, least = 0;
+  for (long n = 1; n <= 64 && (n == 1 || n * 4 <= groups); ++n) {
+    const long cost = (pairs * n + room - 1) / room * ((groups + n * step - 1) / (n * step) + 5) + (n > 1 ? 4 : 0);
+    if (n == 1 || cost < least) { best = n; least = cost; }
+  }
+  return (int)best;
+}
 // Kernel (rows: the waves share the keys), row tiles of 16 (per wave), row blocks, parts that the keys are split into, and what the workspace holds: partial
 // results, then (block > 0) bits of the chosen blocks and their bounds.
 inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int block, int cus) {
@@ -47,13 +60,7 @@ inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int 
   p.mt = p.rows ? (R > 64 ? 2 : 1) : (grouped ? (R + 15) / 16 : 1);
   const int per = p.rows ? 64 * p.mt : (grouped ? 64 : 16);
   p.blocks = (R + per - 1) / per;
-  const long pairs = (long)B * c.n_kv_heads * p.blocks, groups = (c.capacity + 31) / 32;
-  // as many parts as give each CU the workgroups that its registers let run at once (fp32 rows: four; 64 rows that share 128-wide keys: three)
-  const int side = !grouped ? 4 : (p.rows && p.mt == 1 ? 3 : 2);
-  long n = ((long)side * cus + pairs - 1) / pairs, most = groups / 8;
-  n = n < most ? n : most;
-  n = n < 64 ? n : 64;
-  p.nsplit = n < 1 ? 1 : (int)n;
+  p.nsplit = split_of(p, (long)B * c.n_kv_heads * p.blocks, (c.capacity + 31) / 32, grouped, cus);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   p.bytes = p.nsplit > 1 ? up((size_t)B * c.n_kv_heads * p.nsplit * R * (c.head_dim + 2) * 4) : 0;
   if (block && c.capacity / block > 0) {
