@@ -388,8 +388,7 @@ int bpd_cache_store(const bpd_cache* cache, const bpd_rows* k, const bpd_rows* v
  *       capacity, all nodes of a sequence with length[b] < 0.
  *   q, out  rows of n_heads heads (a multiple of the cache's: heads in a row share a key head)
  *   out[b][i][h] = sum_j p_j V_j,  p = softmax of scale * q . K_j over the prefix and node i's ancestors and itself;
- *       0 for absent nodes.  Sums, maxima and weights in fp32; what no node sees does not matter, NaN or not.
- *       (A value that is not finite, in a row that only other nodes of the tree see, may reach all results of its head.)
+ *       0 for absent nodes.  Sums, maxima and weights in fp32.  What a node does not see does not matter to it, finite or not.
  * Chains of one node are plain decoding.  T <= BPD_TREE_MAX; n_heads / n_kv_heads <= 64; B or T of 0 does nothing.
  * Errors: BPD_E_ARG, BPD_E_CAPACITY (workspace), BPD_E_HIP. */
 int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows* out, const int32_t* length,
@@ -399,7 +398,7 @@ int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows
 /* Which blocks of the prefix bpd_sparse_attention sees.  The prefix is cut in blocks of `block` rows, of which
  * n = length / block are complete.  Seen: the first `first`, the last `recent` of them, and of the others
  * the `top` with the largest bound of the scores in them, for each node and key head:
- *     sum over the group's heads of  sum_c max(q_c min_c, q_c max_c),   min, max over the block's keys,
+ *     sum over the group's heads of  sum_c max(q_c min_c, q_c max_c),   min, max over the block's keys (NaN aside),
  * in 64 bits, ties to the lower block, a bound that is NaN last.  Rows behind the last complete block are always seen. */
 typedef struct {
   int32_t block;           /* 32, 64 or 128 rows                                              */

@@ -63,10 +63,11 @@ void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
     if (p.q_f32) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, true, SPARSE>), dim3(p.parts * ((R + 63) / 64), p.kv), dim3(256), 0, s, p);
     else if (plan.mt == 1) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
     else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
-  } else if (plan.mt == 1) attend_few<D, 1, 4, SPARSE>(p, s);
-  else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
-  else if constexpr (D == 64) { if (plan.mt == 3) attend_few<D, 3, 4, SPARSE>(p, s); else attend_few<D, 4, 4, SPARSE>(p, s); }
-
+  } else if constexpr (D == 64) {
+    if (plan.mt == 1) attend_few<D, 1, 4, SPARSE>(p, s);
+    else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
+    else attend_few<D, 3, 4, SPARSE>(p, s);
+  } else attend_few<D, 1, 4, SPARSE>(p, s);
 }
 template <int D>
 void join(const TreeP& p, hipStream_t s) {

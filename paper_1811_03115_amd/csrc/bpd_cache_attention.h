@@ -12,6 +12,8 @@
 #pragma once
 #include "bpd_device.h"
 
+#include <type_traits>
+
 constexpr int TREE_MAX = 64;                     // nodes of a tree: one wave, one 64-bit word of ancestors
 constexpr int TREE_GROUP = 32;                   // keys per group of a cache in operand order
 
@@ -218,8 +220,9 @@ struct TreeTiles {
   }
   // kf, vf: the item's operands; at: this lane's first key among the drafts; edge: whether any key of the item is a draft (the same for the whole wave); vis: whether
   // row t sees the item's committed keys; seen: the drafts that it sees; q(t, x): its operand
-  template <typename Q, typename QL>
-  __device__ __forceinline__ void item(const u32x4 (&kf)[2 * KS], const u32x4 (&vf)[VT], int at, bool edge, const bool (&vis)[MT], const mask64 (&seen)[MT], float scale, const Q& q, const QL& ql) {
+  // SAFE: values one by one (value(key, dimension)), for the keys that a row sees and no others: a product's zero times what is not finite is not zero
+  template <bool SAFE, typename Q, typename QL, typename V>
+  __device__ __forceinline__ void item(const u32x4 (&kf)[2 * KS], const u32x4 (&vf)[VT], int at, bool edge, const bool (&vis)[MT], const mask64 (&seen)[MT], float scale, const Q& q, const QL& ql, const V& value) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       f32x4 s[2];
@@ -264,15 +267,43 @@ struct TreeTiles {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) { const float e = __builtin_amdgcn_exp2f(fmaf(s[u][r], scale, -sub)); pv[4 * u + r] = e; l[t] += e; }
-      bf16x8 ph, pl;
-      tree_pair(pv, ph, pl);
+      if constexpr (SAFE) {
+        const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
+#pragma unroll 1
+        for (int jq = 0; jq < 4; ++jq)
 #pragma unroll
-      for (int x = 0; x < VT; ++x) {
-        const bf16x8 va = __builtin_bit_cast(bf16x8, vf[x]);
-        acc[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, acc[t][x], 0, 0, 0);
-        acc[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, acc[t][x], 0, 0, 0);
+          for (int j = 0; j < 8; ++j) {
+            const float pj = __shfl(pv[j], 16 * jq + lr, 64);
+            const int n = at + 8 * (jq - lq) + j;
+            if (n < 0 ? vis[t] : (n < 64 && (seen[t] >> n & 1))) {
+#pragma unroll
+              for (int x = 0; x < VT; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[t][x][r] = fmaf(pj, value(8 * jq + j, 16 * x + 4 * lq + r), acc[t][x][r]);
+            }
+          }
+      } else {
+        bf16x8 ph, pl;
+        tree_pair(pv, ph, pl);
+#pragma unroll
+        for (int x = 0; x < VT; ++x) {
+          const bf16x8 va = __builtin_bit_cast(bf16x8, vf[x]);
+          acc[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph, acc[t][x], 0, 0, 0);
+          acc[t][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, acc[t][x], 0, 0, 0);
+        }
       }
     }
+  }
+  // Is any of this lane's results not finite?
+  __device__ __forceinline__ bool unclean() const {
+    float z = 0.f;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z = fmaf(acc[t][x][r], 0.f, z);
+    return z != 0.f;                             // (0 times any of them)
   }
 };
 // Values of rows that nobody sees (behind the drafts, absent nodes): their probabilities are zero, their bits unknown.  at: as above
@@ -289,6 +320,10 @@ __device__ __forceinline__ void tree_blank(u32x4 (&vf)[VT], int at, mask64 prese
 #pragma unroll
     for (int x = 0; x < VT; ++x) vf[x][w] &= known;
   }
+}
+// Where dimension c of a key's values lies in a sequence's and head's part of a cache in operand order
+template <int D> __device__ __forceinline__ size_t tree_v_at(int key, int c) {
+  return (size_t)(key >> 5) * (TREE_GROUP * D) + (c >> 4) * 512 + (((key >> 3) & 3) * 16 + (c & 15)) * 8 + (key & 7);
 }
 // Row r of a (sequence, key head) pair: its node, what it sees of the drafts, whether it is there
 __device__ __forceinline__ void tree_row(const TreeP& p, int r, int R, mask64 anc, int& node, mask64& seen, bool& ok) {
@@ -320,19 +355,16 @@ __device__ __forceinline__ void tree_finish4(const TreeP& p, int D, int b, int h
 
 // bf16 heads of D = 64 or 128 in operand order (groups of 32 keys, D x 32 elements of K and as many of V, bpd_attention.h for D = 64; the same with
 // D / 32 steps of K and D / 16 tiles of V otherwise): every operand is one 1 KiB load, nothing of K and V goes through LDS.
-// Up to 64 rows: a workgroup has all of a (sequence, key head) pair's, and one part in nsplit of its items; its NW waves take single items in turn, each with its own
+// Up to 48 rows (16 of 128-wide heads): a workgroup has all of a (sequence, key head) pair's, and one part of its items; its NW waves take single items in turn, each with its own
 // maximum, sum and results, and meet once in LDS.  What bounds it is the stream of K and V; the next item's keys are asked for while this one's values are multiplied.
 template <int D, int MT, int NW, bool QF32, bool SPARSE>
 __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
   constexpr int KS = D / 32, VT = D / 16, GRP = TREE_GROUP * D, SLOTS = NW / 2 > 4 ? NW / 2 : 4;
-  constexpr bool Q_LDS = MT * KS > 8 && !QF32;   // queries of many rows: in LDS, for registers
   __shared__ __attribute__((aligned(16))) f32x4 o_s[SLOTS][VT][64];
   __shared__ float m_s[NW][MT * 16], l_s[NW][MT * 16];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
   __shared__ int sums_s[NW];
   __shared__ unsigned bits_s[SPARSE ? TREE_BLOCKS_MAX / 32 : 1];
-  static_assert(!Q_LDS || MT * KS <= SLOTS * VT, "queries fit where the results meet");
-  u32x4 (*q_s)[KS][64] = (u32x4 (*)[KS][64])&o_s[0][0][0];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lq = lane >> 4;
   const int at_part = blockIdx.x, hk = blockIdx.y, R = p.T * p.G;
   const TreePart part = tree_part(p, at_part, lane);
@@ -355,21 +387,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
   tree_ancestors(p, b, there, lane, anc, ok);
   const mask64 present = __ballot(ok);
   mask64 seen[MT]; int node[MT]; bool row_ok[MT];
-  bf16x8 qh[Q_LDS ? 1 : MT][KS], ql[QF32 ? MT : 1][KS];
+  bf16x8 qh[MT][KS], ql[QF32 ? MT : 1][KS];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int r = 16 * t + lr;
     tree_row(p, r, R, anc, node[t], seen[t], row_ok[t]);
-    if constexpr (Q_LDS) {
-      if (t % NW != wave) continue;
-      bf16x8 lo;
+    bf16x8 lo;
 #pragma unroll
-      for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[0][x], lo); q_s[t][x][lane] = __builtin_bit_cast(u32x4, qh[0][x]); }
-    } else {
-      bf16x8 lo;
-#pragma unroll
-      for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[t][x], lo); if constexpr (QF32) ql[t][x] = lo; }
-    }
+    for (int x = 0; x < KS; ++x) { tree_q_operand(p, b, hk, r, node[t], row_ok[t], 32 * x + 8 * lq, qh[t][x], lo); if constexpr (QF32) ql[t][x] = lo; }
   }
   const int ngr = (len + there + 31) >> 5;
   TreeItems it{0, 0, ngr, nullptr, 1};
@@ -381,11 +406,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
     it.listed = tree_list(picks, p.words, 0, p.T, done, list_s, sums_s, bits_s) * p.bg;
     it.n = it.listed + ngr - it.tail0;
   }
-  if constexpr (Q_LDS) __syncthreads();
   const int i0 = (int)((long)it.n * part.split / part.n), i1 = (int)((long)it.n * (part.split + 1) / part.n);
   TreeTiles<D, MT, QF32> tiles;
   tiles.clear();
-  int i = i0 + wave, g = i < i1 ? __builtin_amdgcn_readfirstlane(it.group(i)) : 0;
   unsigned word[SPARSE ? MT : 1];                // has the row chosen the item's block?
   auto load_words = [&](int ii, int gg) {
     if constexpr (SPARSE) {
@@ -394,29 +417,49 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
       for (int t = 0; t < MT; ++t) word[t] = ii < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
     }
   };
-  if (i < i1) {
-    load_words(i, g);
-    if (SPARSE || part.n > 1) load_k(kf, g);
-  }
-  auto step = [&](u32x4 (&k)[2 * KS], u32x4 (&k_next)[2 * KS]) {
+  // one item, whose keys are here; ahead(): asks for what comes next
+  auto one = [&](auto safe, u32x4 (&k)[2 * KS], int g, const auto& ahead) {
+    constexpr bool SAFE = decltype(safe)::value;
+    if constexpr (!SAFE) {
 #pragma unroll
-    for (int x = 0; x < VT; ++x) vf[x] = Vb[(size_t)g * (GRP / 8) + x * 64];
+      for (int x = 0; x < VT; ++x) vf[x] = Vb[(size_t)g * (GRP / 8) + x * 64];
+    }
     bool vis[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && word[t]; }
-    const int next = i + NW, gn = next < i1 ? __builtin_amdgcn_readfirstlane(it.group(next)) : g;
-    if (next < i1) { load_words(next, gn); load_k(k_next, gn); }
+    ahead();
     const int at = 32 * g + 8 * lq - len;
     const bool edge = 32 * g + 32 > len;
-    if (edge) tree_blank<VT>(vf, at, present);
-    tiles.item(k, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { if constexpr (Q_LDS) return __builtin_bit_cast(bf16x8, q_s[t][x][lane]); else return qh[t][x]; },
-               [&](int t, int x) { return ql[QF32 ? t : 0][x]; });
-    i = next; g = gn;
+    if (!SAFE && edge) tree_blank<VT>(vf, at, present);
+    tiles.template item<SAFE>(k, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; },
+                              [&](int t, int x) { return ql[QF32 ? t : 0][x]; }, [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + tree_v_at<D>(32 * g + j, c)]); });
   };
-  while (i < i1) {                               // (two sets of keys in turn)
-    step(kf, kn);
-    if (i >= i1) break;
-    step(kn, kf);
+  {
+    int i = i0 + wave, g = i < i1 ? __builtin_amdgcn_readfirstlane(it.group(i)) : 0;
+    if (i < i1) {
+      load_words(i, g);
+      if (SPARSE || part.n > 1) load_k(kf, g);
+    }
+    auto step = [&](u32x4 (&k)[2 * KS], u32x4 (&k_next)[2 * KS]) {
+      const int next = i + NW, gn = next < i1 ? __builtin_amdgcn_readfirstlane(it.group(next)) : g;
+      one(std::false_type{}, k, g, [&]() { if (next < i1) { load_words(next, gn); load_k(k_next, gn); } });
+      i = next; g = gn;
+    };
+    while (i < i1) {                             // (two sets of keys in turn)
+      step(kf, kn);
+      if (i >= i1) break;
+      step(kn, kf);
+    }
+  }
+  if (__any(tiles.unclean())) {                  // again, value by value
+    tiles.clear();
+#pragma unroll 1
+    for (int i = i0 + wave; i < i1; i += NW) {
+      const int g = __builtin_amdgcn_readfirstlane(it.group(i));
+      load_words(i, g);
+      load_k(kf, g);
+      one(std::true_type{}, kf, g, [&]() {});
+    }
   }
   // the waves meet: maxima and sums first, then the upper half's results into the lower half's until four are left
 #pragma unroll
@@ -424,7 +467,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
     tiles.l[t] = sum_rows(tiles.l[t]);
     if (lq == 0) { m_s[wave][16 * t + lr] = tiles.m[t]; l_s[wave][16 * t + lr] = tiles.l[t]; }
   }
-  __syncthreads();                               // (and the queries have been read)
+  __syncthreads();
   float M[MT], L[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -466,7 +509,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
   }
 }
 
-// More than 64 rows: the waves have rows of their own, 16 MT each, and walk the same items, which come through LDS, two buffers in turn: an operand is loaded once for 16 MT NW
+// More rows: the waves have rows of their own, 16 MT each, and walk the same items, which come through LDS, two buffers in turn: an operand is loaded once for 16 MT NW
 // rows.  What bounds it is the matrix cores (6 D products per row and 64 keys, with the pairs) and, beside them, the exponentials.
 template <int D, int MT, int NW, bool QF32, bool SPARSE>
 __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p) {
@@ -533,32 +576,40 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
       for (int t = 0; t < MT; ++t) word[t] = ii < it.listed ? picks[(long)node[t] * p.words + (blk >> 5)] >> (blk & 31) & 1 : 1u;
     }
   };
-  int g = 0;
-  if (i0 < i1) { g = __builtin_amdgcn_readfirstlane(it.group(i0)); load_words(i0, g); ask(g); put(0); }
-  __syncthreads();
-  for (int i = i0; i < i1; ++i) {
-    const int buf = (i - i0) & 1;
-    const int gn = i + 1 < i1 ? __builtin_amdgcn_readfirstlane(it.group(i + 1)) : g;
-    unsigned now[SPARSE ? MT : 1];
-#pragma unroll
-    for (int t = 0; t < (SPARSE ? MT : 0); ++t) now[t] = word[t];
-    if (i + 1 < i1) { load_words(i + 1, gn); ask(gn); }
-    u32x4 kf[2 * KS], vf[VT];
-#pragma unroll
-    for (int x = 0; x < 2 * KS; ++x) kf[x] = kv_s[buf][x * 64 + lane];
-#pragma unroll
-    for (int x = 0; x < VT; ++x) vf[x] = kv_s[buf][PIECES + x * 64 + lane];
-    bool vis[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && now[t]; }
-    const int at = 32 * g + 8 * lq - len;
-    const bool edge = 32 * g + 32 > len;
-    if (edge) tree_blank<VT>(vf, at, present);
-    tiles.item(kf, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; }, [&](int t, int x) { return ql[QF32 ? t : 0][x]; });
-    if (i + 1 < i1) put(buf ^ 1);
+  auto walk = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
+    int g = 0;
+    if (i0 < i1) { g = __builtin_amdgcn_readfirstlane(it.group(i0)); load_words(i0, g); ask(g); put(0); }
     __syncthreads();
-    g = gn;
-  }
+    for (int i = i0; i < i1; ++i) {
+      const int buf = (i - i0) & 1;
+      const int gn = i + 1 < i1 ? __builtin_amdgcn_readfirstlane(it.group(i + 1)) : g;
+      unsigned now[SPARSE ? MT : 1];
+#pragma unroll
+      for (int t = 0; t < (SPARSE ? MT : 0); ++t) now[t] = word[t];
+      if (i + 1 < i1) { load_words(i + 1, gn); ask(gn); }
+      u32x4 kf[2 * KS], vf[VT];
+#pragma unroll
+      for (int x = 0; x < 2 * KS; ++x) kf[x] = kv_s[buf][x * 64 + lane];
+      if constexpr (!SAFE) {
+#pragma unroll
+        for (int x = 0; x < VT; ++x) vf[x] = kv_s[buf][PIECES + x * 64 + lane];
+      }
+      bool vis[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) { vis[t] = row_ok[t]; if constexpr (SPARSE) vis[t] = vis[t] && now[t]; }
+      const int at = 32 * g + 8 * lq - len;
+      const bool edge = 32 * g + 32 > len;
+      if (!SAFE && edge) tree_blank<VT>(vf, at, present);
+      tiles.template item<SAFE>(kf, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; }, [&](int t, int x) { return ql[QF32 ? t : 0][x]; },
+                                [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + tree_v_at<D>(32 * g + j, c)]); });
+      if (i + 1 < i1) put(buf ^ 1);
+      __syncthreads();
+      g = gn;
+    }
+  };
+  walk(std::false_type{});
+  if (__syncthreads_or(tiles.unclean())) { tiles.clear(); walk(std::true_type{}); }
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const float L = sum_rows(tiles.l[t]);
@@ -615,64 +666,91 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
   const long own = (long)tree_cache(p, b) * p.cap * stride + hk * D;
   const S* Kb = (const S*)p.K + own;
   const S* Vb = (const S*)p.V + own;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run, l_run;
   f32x4 acc[VT];
+  auto walk = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
+    m_run = -INFINITY; l_run = 0.f;
 #pragma unroll
-  for (int x = 0; x < VT; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = i0 + wave; i < i1; i += 4) {
-    const int g = __builtin_amdgcn_readfirstlane(it.group(i));
-    bool vis = row_ok;
-    if constexpr (SPARSE) {
-      if (i < it.listed) { const int blk = g / p.bg; vis = vis && (picks[(long)node * p.words + (blk >> 5)] >> (blk & 31) & 1); }
+    for (int x = 0; x < VT; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = i0 + wave; i < i1; i += 4) {
+      const int g = __builtin_amdgcn_readfirstlane(it.group(i));
+      bool vis = row_ok;
+      if constexpr (SPARSE) {
+        if (i < it.listed) { const int blk = g / p.bg; vis = vis && (picks[(long)node * p.words + (blk >> 5)] >> (blk & 31) & 1); }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int k0 = 32 * g + 16 * u, end = len + there;
+        if (k0 >= end) break;                      // (the same for the whole wave)
+        const int key = min(k0 + lr, end - 1);     // K: this lane's key; past the last one nothing is read
+        f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < VT; ++x) {
+          const S* kp = Kb + key * stride + 16 * x + 4 * lq;
+          float kv[4];
+          if constexpr (sizeof(S) == 4) { const f32x4 w = *(const f32x4*)kp; kv[0] = w[0]; kv[1] = w[1]; kv[2] = w[2]; kv[3] = w[3]; }
+          else { const u32x2 w = *(const u32x2*)kp; kv[0] = __uint_as_float(w[0] << 16); kv[1] = __uint_as_float(w[0] & 0xFFFF0000u); kv[2] = __uint_as_float(w[1] << 16); kv[3] = __uint_as_float(w[1] & 0xFFFF0000u); }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[j], q[x][j], a, 0, 0, 0);
+        }
+        float vv[VT][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int kk = k0 + 4 * lq + r, n = kk - len;
+          const bool known = kk < len || (n < 64 && kk < end && (present >> n & 1));
+#pragma unroll
+          for (int x = 0; x < VT; ++x) { const float v = to_f<S>(Vb[min(kk, end - 1) * stride + 16 * x + lr]); vv[x][r] = known ? v : 0.f; }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int n = k0 + 4 * lq + r - len;
+          const bool in = n < 0 ? vis : (n < 64 && (seen >> n & 1));
+          a[r] = in ? a[r] * p.scale : -INFINITY;
+          mx = fmaxf(mx, a[r]);
+        }
+        mx = max_rows(mx);
+        const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { a[r] = exp2f(a[r] - m_use); sum += a[r]; }
+        sum = sum_rows(sum);
+        const float alpha = exp2f(m_run - m_use);
+        l_run = l_run * alpha + sum;
+        m_run = m_new;
+#pragma unroll
+        for (int x = 0; x < VT; ++x) acc[x] *= alpha;
+        if constexpr (SAFE) {                    // (as TreeTiles::item)
+#pragma unroll 1
+          for (int jq = 0; jq < 4; ++jq)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float pj = __shfl(a[j], 16 * jq + lr, 64);
+              const int kk = k0 + 4 * jq + j, n = kk - len;
+              if (n < 0 ? vis : (n < 64 && (seen >> n & 1))) {
+#pragma unroll
+                for (int x = 0; x < VT; ++x)
+#pragma unroll
+                  for (int r = 0; r < 4; ++r) acc[x][r] = fmaf(pj, to_f<S>(Vb[kk * stride + 16 * x + 4 * lq + r]), acc[x][r]);
+              }
+            }
+        } else {
+#pragma unroll
+          for (int x = 0; x < VT; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[x][r], a[r], acc[x], 0, 0, 0);
+        }
+      }
     }
+  };
+  walk(std::false_type{});
+  float z = 0.f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int k0 = 32 * g + 16 * u, end = len + there;
-      if (k0 >= end) break;                      // (the same for the whole wave)
-      const int key = min(k0 + lr, end - 1);     // K: this lane's key; past the last one nothing is read
-      f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < VT; ++x)
 #pragma unroll
-      for (int x = 0; x < VT; ++x) {
-        const S* kp = Kb + key * stride + 16 * x + 4 * lq;
-        float kv[4];
-        if constexpr (sizeof(S) == 4) { const f32x4 w = *(const f32x4*)kp; kv[0] = w[0]; kv[1] = w[1]; kv[2] = w[2]; kv[3] = w[3]; }
-        else { const u32x2 w = *(const u32x2*)kp; kv[0] = __uint_as_float(w[0] << 16); kv[1] = __uint_as_float(w[0] & 0xFFFF0000u); kv[2] = __uint_as_float(w[1] << 16); kv[3] = __uint_as_float(w[1] & 0xFFFF0000u); }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[j], q[x][j], a, 0, 0, 0);
-      }
-      float vv[VT][4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int kk = k0 + 4 * lq + r, n = kk - len;
-        const bool known = kk < len || (n < 64 && kk < end && (present >> n & 1));
-#pragma unroll
-        for (int x = 0; x < VT; ++x) { const float v = to_f<S>(Vb[min(kk, end - 1) * stride + 16 * x + lr]); vv[x][r] = known ? v : 0.f; }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int n = k0 + 4 * lq + r - len;
-        const bool in = n < 0 ? vis : (n < 64 && (seen >> n & 1));
-        a[r] = in ? a[r] * p.scale : -INFINITY;
-        mx = fmaxf(mx, a[r]);
-      }
-      mx = max_rows(mx);
-      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-      float sum = 0.f;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) { a[r] = exp2f(a[r] - m_use); sum += a[r]; }
-      sum = sum_rows(sum);
-      const float alpha = exp2f(m_run - m_use);
-      l_run = l_run * alpha + sum;
-      m_run = m_new;
-#pragma unroll
-      for (int x = 0; x < VT; ++x) {
-        acc[x] *= alpha;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[x][r], a[r], acc[x], 0, 0, 0);
-      }
-    }
-  }
+    for (int r = 0; r < 4; ++r) z = fmaf(acc[x][r], 0.f, z);
+  if (__any(z != 0.f)) walk(std::true_type{});
   if (lq == 0) { m_s[wave][lr] = m_run; l_s[wave][lr] = l_run; }
 #pragma unroll
   for (int x = 0; x < VT; ++x) o_s[wave][x][lane] = acc[x];

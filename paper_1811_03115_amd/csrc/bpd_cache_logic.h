@@ -56,9 +56,9 @@ inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int 
   TreePlan p{};
   const int R = T * (heads / c.n_kv_heads);
   const bool grouped = cache_grouped(c);
-  p.rows = grouped && R > (c.head_dim == 64 ? 64 : 32);
+  p.rows = grouped && R > (c.head_dim == 64 ? 48 : 16);        // (more tiles than that in one wave's registers: spills)
   p.mt = p.rows ? (R > 64 ? 2 : 1) : (grouped ? (R + 15) / 16 : 1);
-  const int per = p.rows ? 64 * p.mt : (grouped ? 64 : 16);
+  const int per = p.rows ? 64 * p.mt : (grouped ? 48 : 16);
   p.blocks = (R + per - 1) / per;
   p.nsplit = split_of(p, (long)B * c.n_kv_heads * p.blocks, (c.capacity + 31) / 32, grouped, cus);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };

@@ -56,7 +56,7 @@ def same_bits(a, b):
 SHAPES = [
     (1, 1, 1, [0], 32, "chain"), (2, 1, 1, [1, 31], 32, "chain"), (1, 1, 3, [29, 30, -1, 32], 32, "chain"), (3, 1, 10, [0, 33, 95, 64], 128, "tree"),
     (2, 4, 12, [130, 7], 160, "odd"), (1, 8, 64, [100], 192, "tree"), (5, 1, 16, [31, 32, 33], 64, "odd"), (1, 3, 11, [200, 255], 288, "tree"),
-    (2, 1, 7, [700, 1017, 1024, 3], 1024, "tree"), (1, 1, 33, [2000], 2048, "odd"), (1, 64, 1, [77], 96, "chain"), (2, 2, 64, [1500, 0], 1600, "odd"),
+    (2, 1, 7, [700, 1017, 1024, 3], 1024, "tree"), (1, 3, 16, [90, 31], 128, "odd"), (1, 7, 7, [500], 544, "tree"), (1, 1, 17, [5000, 40], 5056, "tree"), (1, 1, 3, [4700, 4097, 1, -1], 4704, "tree"), (1, 1, 33, [2000], 2048, "odd"), (1, 64, 1, [77], 96, "chain"), (2, 2, 64, [1500, 0], 1600, "odd"),
 ]
 
 
@@ -143,6 +143,50 @@ def test_extreme_scores(d, dtype):
     want, off, _ = ref.attention(q, k, v, lengths, parent)
     got = bpd.bpd_tree_attention(tuple(cuda(x) for x in ref.pack(k, v)), cuda(q), ints(lengths), cuda(parent))
     ref.check(got, want, off)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16), (F32, 64), (BF, 16)], ids=lambda x: str(x).replace("torch.", ""))
+@pytest.mark.parametrize("kv,g,t,n,cap", [(2, 1, 9, 70, 96), (1, 2, 13, 400, 448), (1, 3, 20, 700, 1024), (1, 8, 12, 333, 1024), (1, 1, 2, 31, 64)])
+def test_what_others_see_does_not_matter(dtype, d, kv, g, t, n, cap):
+    """Keys and values that are not finite, in drafts of other branches, in absent nodes and in blocks that only other nodes chose: results as without them; who sees them gets what
+    the formula gives."""
+    rng = np.random.default_rng(d + t)
+    parent = np.array([[-1] + [max(0, i - 2) for i in range(1, t)]], np.int32)          # two branches
+    if t > 3:
+        parent[0, t - 1] = -3
+    k, v = cache_of(rng, 1, cap, kv, d, dtype, [n], t, parent)
+    q = rows(rng, 1, t, kv * g, d, dtype=dtype)
+    bad = t - 2 if t > 3 else t - 1                # a leaf
+    sees = [i for i, a in enumerate(ref.ancestors(parent[0], t)) if a is not None and bad in a]
+    clean = ref.attention(q, k, v, [n], parent)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        k2, v2 = k.clone(), v.clone()
+        v2[0, n + bad, :, ::3] = value
+        if value != value:
+            k2[0, n + bad, :, 5] = value
+        got = bpd.bpd_tree_attention(tuple(cuda(x) for x in ref.pack(k2, v2)), cuda(q), ints([n]), cuda(parent)).cpu()
+        others = [i for i in range(t) if i not in sees]
+        ref.check(got[:, others], clean[0][:, others], clean[1][:, others], what=str(value))
+        want = ref.attention(q, k2, v2, [n], parent)[0]
+        hit = ~torch.isfinite(want)
+        assert hit.any() and torch.equal(torch.isnan(got.double()), torch.isnan(want)) and torch.equal(got.double()[hit & ~torch.isnan(want)], want[hit & ~torch.isnan(want)])
+        # a block that some of the nodes choose
+        what = dict(block=32, first=0, recent=0, top=1)
+        _, _, picks = ref.attention(q, k, v, [n], parent, blocks=what)
+        words = picks.numpy().view(np.uint32)[0, 0]
+        block = next((j for j in range(n // 32) if 0 < sum(int(w[j // 32]) >> (j % 32) & 1 for w in words) < len(words)), None)
+        if block is None or kv > 1:
+            continue
+        v2 = v.clone()
+        v2[0, block * 32 + 3, 0, 1::2] = value
+        cache = tuple(cuda(x) for x in ref.pack(k, v2))
+        got, chosen = bpd.bpd_sparse_attention(cache, cuda(q), ints([n]), binding.new_summaries(cache, 32), parent=cuda(parent), **what)
+        assert torch.equal(chosen.cpu(), picks)
+        want, off, _ = ref.attention(q, k, v2, [n], parent, blocks=what)
+        fine = torch.isfinite(want).all(3).all(2)[0]
+        assert fine.any() and not fine.all()
+        ref.check(got[:, fine], want[:, fine], off[:, fine])
+        assert torch.equal(torch.isnan(got.cpu().double()), torch.isnan(want))
 
 
 def test_far_offsets():
