@@ -1048,6 +1048,7 @@ void lean_ffn(bpd_ctx* ctx, float* x, LnW ln, void* xn, const void* w1, const fl
   lean_residual(ctx, hidden, F, w2, b2, M, x);
 }
 
+bool capturing(const bpd_ctx* ctx);
 // The decoder's self-attention caches as the cache operators take them: all layers, or layer l
 bpd_cache self_cache(const bpd_ctx* ctx, int l = -1) {
   const bpd_config& c = ctx->cfg;
@@ -1056,16 +1057,18 @@ bpd_cache self_cache(const bpd_ctx* ctx, int l = -1) {
   return bpd_cache{(char*)ctx->lay.selfK + at, (char*)ctx->lay.selfV + at, c.dtype, l < 0 ? c.n_dec_layers : 1, c.max_batch, c.n_heads, c.d_model / c.n_heads, (int32_t)rows};
 }
 // Self-attention of R rows per sequence, whose keys and values are in layer l's cache: of a chain over all of it, or of a tree, or over chosen blocks
-void self_attention(bpd_ctx* ctx, int l, const void* Kl, const void* Vl, int slots, int B, int R, const int* base, const int* seq, bool packed) {
+// (own_keys: neither; also the first invocation, whose one row sees itself, and whose launches are recorded and outlive the setting and its buffer)
+void self_attention(bpd_ctx* ctx, int l, const void* Kl, const void* Vl, int slots, int B, int R, const int* base, const int* seq, bool packed, bool own_keys) {
   const Layout& L = ctx->lay;
-  if (!ctx->tree && !ctx->sparse.block) { attention(ctx, L.q, Kl, Vl, L.attn, slots, B, R, base, 1, seq, packed); return; }
+  if (own_keys) { attention(ctx, L.q, Kl, Vl, L.attn, slots, B, R, base, 1, seq, packed); return; }
   const int dh = ctx->cfg.d_model / ctx->cfg.n_heads;
   BlockAttention a{self_cache(ctx, l), L.q, L.attn, packed, base, seq, ctx->tree, B, R, ctx->cfg.n_heads, 1.0f / sqrtf((float)dh), nullptr, 0,
                    L.attn_part, (size_t)ATTN_PART_SLOTS * 16 * (dh + 2) * 4, ctx->num_cus};
   bpd_blocks blocks = ctx->sparse;
   if (blocks.block) {
     blocks.summaries = (char*)blocks.summaries + (size_t)l * summaries_elements(a.cache, blocks.block) * cache_element(a.cache);
-    a.blocks = &blocks; a.added = ctx->cfg.k_max;         // (no step commits more, and each summarises what the one before has left)
+    // No step commits more than k_max rows, and each summarises what the one before has left; a caller's replays may have been of steps that did not.
+    a.blocks = &blocks; a.added = ctx->replayable && !capturing(ctx) ? -1 : ctx->cfg.k_max;
     a.scratch = ctx->sparse_scratch; a.scratch_bytes = ctx->sparse_scratch_bytes;
   }
   launch_block_attention(a, ctx->stream);
@@ -1107,7 +1110,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
     ctx->x_ready_k = 0;
     xs = have_x && !sp;
     if (!have_x) embed(ctx, L.P, c.k_max, base, R, M, L.pos_tgt, L.x, zero_input, L.keys, (int)nk, seq);
-    const bool own_keys = !ctx->tree && !ctx->sparse.block;       // (the kernels of all layers attend to all keys of a chain)
+    const bool own_keys = zero_input || (!ctx->tree && !ctx->sparse.block);       // (the kernels of all layers attend to all keys of a chain)
     const bool stack = own_keys && M <= 16 && (lean || sp) && stack_usable(ctx, B, R);
     const int way = stack || !lean || !own_keys ? LAYERS_CHAIN : layers_way(ctx, B, R);
     const bool one = way != LAYERS_CHAIN;
@@ -1128,7 +1131,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
           lean_ln_gemm<RG_QKV>(ctx, L.x, w.ln1, L.xn, q);
         } else {
           lean_ln_gemm<RG_QKV>(ctx, L.x, w.ln1, L.xn, rg_kv(ctx, nullptr, w.wqkv, M, 3 * d, kv));
-          self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean);
+          self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean, own_keys);
         }
         lean_residual(ctx, L.attn, d, w.wo, nullptr, M, L.x);
         if (qproj) {
@@ -1144,7 +1147,7 @@ int forward(bpd_ctx* ctx, int R, int k, int zero_input, float* logits) {
       }
       // self-attention sublayer: K/V of the block rows go straight into the cache at L_b + i'
       gemm_ln(ctx, L.x, w.ln1, L.xn, nullptr, gp(L.xn, d, w.wqkv, 3 * d, M, 3 * d, d), kv, sp, xs, folds ? &w.f_qkv : nullptr);
-      self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean);
+      self_attention(ctx, l, Kl, Vl, slots, B, R, base, seq, lean, own_keys);
       xs = gemm(ctx, gp(L.attn, d, w.wo, d, M, d, d), residual(nullptr, d));
       // cross-attention sublayer over the encoder memory
       if (qproj) {

@@ -189,6 +189,30 @@ def test_what_others_see_does_not_matter(dtype, d, kv, g, t, n, cap):
         assert torch.equal(torch.isnan(got.cpu().double()), torch.isnan(want))
 
 
+def test_many_rows_and_fewer_sequences():
+    """64 nodes times 64 heads on a key head; fewer sequences than the cache has; lengths past its end; results in the queries' place."""
+    rng = np.random.default_rng(12)
+    for d, dtype in ((64, BF), (128, BF), (16, F32)):
+        b, t, kv, g, cap, lengths = 2, 64, 1, 64, 160, [90, 161]
+        k, v = rows(rng, 4, cap, kv, d, dtype=dtype), rows(rng, 4, cap, kv, d, dtype=dtype)
+        q, parent = rows(rng, b, t, kv * g, d, dtype=dtype), tree(rng, b, t, "tree")
+        want, off, _ = ref.attention(q, k[:b], v[:b], lengths, parent)
+        out = cuda(q).clone()
+        got = bpd.bpd_tree_attention(tuple(cuda(x) for x in ref.pack(k, v)), out, ints(lengths), cuda(parent), out=out)
+        ref.check(got, want, off)
+        assert not bool(got[1].any())
+
+
+def test_negative_and_zero_scales():
+    rng = np.random.default_rng(13)
+    for d, dtype in ((64, BF), (128, BF), (16, F32)):
+        k, v = rows(rng, 1, 320, 1, d, dtype=dtype), rows(rng, 1, 320, 1, d, dtype=dtype)
+        q = rows(rng, 1, 5, 2, d, dtype=dtype)
+        for scale in (-0.3, 0.0, 2.0, 1e-20):
+            want, off, _ = ref.attention(q, k, v, [300], None, scale=scale)
+            ref.check(bpd.bpd_tree_attention(tuple(cuda(x) for x in ref.pack(k, v)), cuda(q), ints([300]), scale=scale), want, off, what=str(scale))
+
+
 def test_far_offsets():
     """A cache of more than 2^32 bytes: the last sequence's rows are read, stored and moved where they are."""
     rng = np.random.default_rng(8)

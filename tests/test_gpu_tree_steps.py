@@ -21,8 +21,9 @@ BF16 = wl.Config("ts-bf16", 63, 1, 2, 128, 2, 512, 272, 8, 5, 12, 40, "bf16", 2,
 BF16_ONE = wl.Config("ts-bf16-one", 64, 1, 2, 128, 2, 512, 272, 10, 1, 12, 60, "bf16", 2, src_kind="uniform3")
 BF16_ODD = wl.Config("ts-bf16-odd", 65, 1, 2, 192, 3, 288, 272, 7, 3, 12, 40, "bf16", 2, src_kind="uniform3")              # 64-wide heads, other widths: one to two row tiles
 BF16_16 = wl.Config("ts-bf16-16", 66, 1, 2, 64, 4, 128, 272, 6, 4, 12, 40, "bf16", 2, src_kind="uniform3")                # 16-wide heads
+BF16_16_LEAN = wl.Config("ts-bf16-16-lean", 71, 1, 2, 128, 8, 512, 272, 8, 4, 12, 40, "bf16", 2, src_kind="uniform3")         # 16-wide heads, kernels of constant K
 LAYERS = wl.Config("ts-layers", 67, 1, 2, 512, 8, 2048, 512, 8, 2, 12, 40, "bf16", 2, src_kind="uniform3")                # the shape whose chains run as one kernel
-ALL = [F32, F32_LONG, BF16, BF16_ONE, BF16_ODD, BF16_16, LAYERS]
+ALL = [F32, F32_LONG, BF16, BF16_ONE, BF16_ODD, BF16_16, BF16_16_LEAN, LAYERS]
 
 
 def trees(k, seed, n=3):
@@ -350,6 +351,59 @@ def test_sparse_decode_with_ended_sequences():
         z = model.all_position_logits(model.encode(src[b, :n[b]]), got[:-1].tolist(), k=1)[:, 0]
         check_argmax(got, z, tol_of(cfg), f"tokens of {b}")
     assert st.finished == cfg.batch
+
+
+@pytest.mark.parametrize("cfg", [BF16, BF16_ODD, F32_LONG], ids=lambda c: c.name)
+def test_encodes_recorded_under_the_setting(cfg):
+    """Encodes that come again are recorded: under the setting they are those without it, and outlive its buffer."""
+    weights = wl.make_weights(cfg)
+    src, n = wl.make_sources(cfg)
+    plain, ctx = gpu_context(cfg, weights), gpu_context(cfg, weights)
+    plain.bpd_encode(src, n)
+    want = [np.array(x) for x in plain.bpd_get_state()]
+    ctx.bpd_set_sparse_attention(32, 1, 1, 4)
+    for _ in range(10):
+        ctx.bpd_encode(src, n)
+    ctx.bpd_step(cfg.k)
+    ctx.bpd_set_sparse_attention(0)
+    torch.cuda.synchronize()
+    junk = torch.full((1 << 22,), float("nan"), device="cuda")
+    for _ in range(2):
+        ctx.bpd_encode(src, n)
+        for x, y in zip(want, ctx.bpd_get_state()):
+            np.testing.assert_array_equal(x, y)
+    assert bool(torch.isnan(junk).all())
+
+
+def test_captured_sparse_steps():
+    """Steps by chosen blocks in a graph, replayed, with direct steps in between, against direct calls alone."""
+    cfg = F32_LONG
+    weights = wl.make_weights(cfg)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctxs = [binding.Context(binding.config_from_workload(cfg), stream=side) for _ in range(2)]
+    src, n = wl.make_sources(cfg)
+    whole = torch.full((cfg.batch,), cfg.k, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    for c in ctxs:
+        c.bpd_load_weights(weights)
+        c.bpd_set_sparse_attention(32, 1, 1, 1)
+        c.bpd_encode(src, n)
+        c.bpd_step(cfg.k, whole)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        ctxs[0].bpd_step(cfg.k, whole)
+    for step in range(25):
+        with torch.cuda.stream(side):
+            graph.replay()
+        ctxs[1].bpd_step(cfg.k, whole)
+        if step % 6 == 5:
+            for c in ctxs:
+                c.bpd_step(cfg.k, whole)
+        side.synchronize()
+        for x, y in zip(ctxs[0].bpd_get_state(), ctxs[1].bpd_get_state()):
+            np.testing.assert_array_equal(x, y, err_msg=f"step {step}")
 
 
 def test_sparse_refusals():
