@@ -623,7 +623,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
 // dimension of its own from each of its four keys, and nothing is transposed.
 template <typename S, int D, bool SPARSE>
 __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
-  constexpr int VT = D / 16;
+  constexpr int VT = D / 16, CH = VT;
   __shared__ __attribute__((aligned(16))) f32x4 o_s[4][VT][64];
   __shared__ float m_s[4][16], l_s[4][16];
   __shared__ unsigned short list_s[SPARSE ? TREE_BLOCKS_MAX : 1];
@@ -684,7 +684,9 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
         const int k0 = 32 * g + 16 * u, end = len + there;
         if (k0 >= end) break;                      // (the same for the whole wave)
         const int key = min(k0 + lr, end - 1);     // K: this lane's key; past the last one nothing is read
-        f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 part_a[CH];                          // (sums of an eighth of the dimensions, then of those: a chain over 128 of them is off by three times as much)
+#pragma unroll
+        for (int x = 0; x < CH; ++x) part_a[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < VT; ++x) {
           const S* kp = Kb + key * stride + 16 * x + 4 * lq;
@@ -692,8 +694,11 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
           if constexpr (sizeof(S) == 4) { const f32x4 w = *(const f32x4*)kp; kv[0] = w[0]; kv[1] = w[1]; kv[2] = w[2]; kv[3] = w[3]; }
           else { const u32x2 w = *(const u32x2*)kp; kv[0] = __uint_as_float(w[0] << 16); kv[1] = __uint_as_float(w[0] & 0xFFFF0000u); kv[2] = __uint_as_float(w[1] << 16); kv[3] = __uint_as_float(w[1] & 0xFFFF0000u); }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[j], q[x][j], a, 0, 0, 0);
+          for (int j = 0; j < 4; ++j) part_a[x % CH] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[j], q[x][j], part_a[x % CH], 0, 0, 0);
         }
+        f32x4 a = part_a[0];
+        if constexpr (CH == 4) a = (part_a[0] + part_a[1]) + (part_a[2] + part_a[3]);
+        if constexpr (CH == 8) a = ((part_a[0] + part_a[1]) + (part_a[2] + part_a[3])) + ((part_a[4] + part_a[5]) + (part_a[6] + part_a[7]));
         float vv[VT][4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -707,14 +712,15 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
         for (int r = 0; r < 4; ++r) {
           const int n = k0 + 4 * lq + r - len;
           const bool in = n < 0 ? vis : (n < 64 && (seen >> n & 1));
-          a[r] = in ? a[r] * p.scale : -INFINITY;
+          a[r] = in ? a[r] : -INFINITY;
           mx = fmaxf(mx, a[r]);
         }
-        mx = max_rows(mx);
+        // (scaled in the difference: the rounding of m is the same factor in every weight, and no other is made)
+        mx = max_rows(mx) * p.scale;
         const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) { a[r] = exp2f(a[r] - m_use); sum += a[r]; }
+        for (int r = 0; r < 4; ++r) { a[r] = exp2f(fmaf(a[r], p.scale, -m_use)); sum += a[r]; }
         sum = sum_rows(sum);
         const float alpha = exp2f(m_run - m_use);
         l_run = l_run * alpha + sum;
