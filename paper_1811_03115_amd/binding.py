@@ -281,7 +281,7 @@ def _attention(cache, layer, q, length, parent, scale, out, workspace, block):
     if q.get_device() != device:
         raise _bad("q and the cache are on different devices")
     if out is None:
-        out = _torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = _torch.empty_like(q) if q.is_contiguous() else _torch.empty(shape, dtype=q.dtype, device=q.device)
     elif out.shape != shape or out.get_device() != device:
         raise _bad("out: the shape and device of q")
     length_p, parent_p = _int(device, (b,), "length", length), _int(device, (b, t), "parent", parent)
@@ -562,10 +562,8 @@ class Context:
             raise _bad("parent: [B, T]")
         b, t = shape
         one = (b,)
-        if out is None:                            # (a piece of memory for the four of them)
-            path, accepted, following, new_length = _torch.empty(b * (t + 3), dtype=_torch.int32, device=parent.device).split((b * t, b, b, b))
-            path = path.view(shape)
-            out = (path, accepted, following, new_length)
+        if out is None:
+            out = (_torch.empty_like(parent), _torch.empty_like(length), _torch.empty_like(length), _torch.empty_like(length))
         path, accepted, following, new_length = out
         c = None
         if cache is not None:

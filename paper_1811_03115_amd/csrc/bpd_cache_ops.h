@@ -58,16 +58,28 @@ __global__ __launch_bounds__(256) void store_groups_kernel(StoreP p) {
   const long ks = (long)layer * p.k.layer + (long)b * p.k.seq + (long)h * p.k.head, vs = (long)layer * p.v.layer + (long)b * p.v.seq + (long)h * p.v.head;
   const size_t part = (size_t)layer * p.layer + ((size_t)b * p.kv + h) * p.cap * D + (size_t)key0 * D;
   bf16_t *K = (bf16_t*)p.K + part, *V = (bf16_t*)p.V + part;
-  for (int x = tid; x < PIECES; x += 256) {      // V's rows: D / 8 pieces each
-    const int key = x / (D / 8), c = x % (D / 8) * 8, i = key0 + key - first;
-    u32x4 w = u32x4{0, 0, 0, 0};
-    if (i >= lo && i < hi) w = rows_bf16x8(p.v, vs + (long)i * p.v.row + c);
-    *(u32x4*)&v_s[key][c] = w;
+  constexpr int N = PIECES / 256;
+  u32x4 v[N], k[N];
+  bool there[N];                                 // (all loads first: four sequences of up to 8100 rows, 8 heads of 128 32.8 us instead of 34.3)
+#pragma unroll
+  for (int j = 0; j < N; ++j) {                  // V's rows: D / 8 pieces each
+    const int x = j * 256 + tid, key = x / (D / 8), i = key0 + key - first;
+    v[j] = u32x4{0, 0, 0, 0};
+    if (i >= lo && i < hi) v[j] = rows_bf16x8(p.v, vs + (long)i * p.v.row + x % (D / 8) * 8);
   }
-  for (int x = tid; x < PIECES; x += 256) {      // [t][s][q][a][r]
-    const int r = x & 3, a = (x >> 2) & 3, q = (x >> 4) & 3, s = (x >> 6) % (D / 32), t = (x >> 6) / (D / 32), i = key0 + 8 * a + 4 * t + r - first;
-    if (i >= lo && i < hi) *(u32x4*)(K + x * 8) = rows_bf16x8(p.k, ks + (long)i * p.k.row + 32 * s + 8 * q);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {                  // [t][s][q][a][r]
+    const int x = j * 256 + tid, r = x & 3, a = (x >> 2) & 3, q = (x >> 4) & 3, s = (x >> 6) % (D / 32), t = (x >> 6) / (D / 32), i = key0 + 8 * a + 4 * t + r - first;
+    there[j] = i >= lo && i < hi;
+    if (there[j]) k[j] = rows_bf16x8(p.k, ks + (long)i * p.k.row + 32 * s + 8 * q);
   }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int x = j * 256 + tid;
+    *(u32x4*)&v_s[x / (D / 8)][x % (D / 8) * 8] = v[j];
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) if (there[j]) *(u32x4*)(K + (j * 256 + tid) * 8) = k[j];
   __syncthreads();
   for (int x = tid; x < PIECES; x += 256) {      // [tile][q][c]
     const int c = x & 15, q = (x >> 4) & 3, t = x >> 6, i = key0 + 8 * q - first;
