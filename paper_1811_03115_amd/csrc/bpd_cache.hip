@@ -224,7 +224,7 @@ int bpd_cache_store(const bpd_cache* c, const bpd_rows* k, const bpd_rows* v, co
     if (c->head_dim == 64) hipLaunchKernelGGL(store_groups_kernel<64>, grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(store_groups_kernel<128>, grid, dim3(256), 0, s, p);
   } else {
-    const dim3 grid(T, 1, B * c->n_layers);
+    const dim3 grid(std::min(T, 1 << 16), 1, B * c->n_layers);           // (2^24 rows would be 2^32 threads, one more than a launch has)
     if (c->dtype == BPD_F32) hipLaunchKernelGGL(store_rows_kernel<float>, grid, dim3(256), 0, s, p, c->head_dim);
     else hipLaunchKernelGGL(store_rows_kernel<bf16_t>, grid, dim3(256), 0, s, p, c->head_dim);
   }

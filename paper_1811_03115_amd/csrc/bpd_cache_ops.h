@@ -100,11 +100,10 @@ __global__ __launch_bounds__(256) void store_groups_kernel(StoreP p) {
 // Caches whose rows lie as they are: an element per thread
 template <typename S>
 __global__ __launch_bounds__(256) void store_rows_kernel(StoreP p, int D) {
-  const int layer = blockIdx.z / p.B, b = blockIdx.z - layer * p.B, i = blockIdx.x;
+  const int layer = blockIdx.z / p.B, b = blockIdx.z - layer * p.B;
   int first, lo, hi;
   store_extent(p, b, first, lo, hi);
-  if (i < lo || i >= hi) return;
-  for (int x = threadIdx.x; x < p.kv * D; x += 256) {
+  for (int i = lo + blockIdx.x; i < hi; i += gridDim.x) for (int x = threadIdx.x; x < p.kv * D; x += 256) {
     const int h = x / D, c = x - h * D;
     const size_t to = (size_t)layer * p.layer + ((size_t)b * p.cap + first + i) * p.kv * D + x;
     const long ka = (long)layer * p.k.layer + (long)b * p.k.seq + (long)i * p.k.row + (long)h * p.k.head + c, va = (long)layer * p.v.layer + (long)b * p.v.seq + (long)i * p.v.row + (long)h * p.v.head + c;

@@ -238,6 +238,21 @@ def test_far_offsets():
 
 # ------------------------------------------------------------------------------------------------ store
 
+def test_largest_capacity():
+    """2^24 rows, all of them the same row, stored by one call and attended to: sums of 2^24 powers of two of one size are exact in 32 bits, and what
+    is left is the rounding of a quotient, less than half a step of bf16."""
+    n = 1 << 24
+    cache = binding.new_cache(1, 1, 16, n)
+    row = torch.tensor([2.0 ** (i % 5 - 2) * (-1) ** (i // 5) for i in range(16)], dtype=BF, device="cuda")
+    bpd.bpd_cache_store(cache, row.expand(1, n, 1, 16), row.expand(1, n, 1, 16), ints([0]))
+    for x in cache:
+        assert bool((x.view(n, 16) == row).all())
+    for length, t in ((n, 1), (n - 2, 2)):
+        out = bpd.bpd_tree_attention(cache, torch.zeros(1, t, 1, 16, dtype=BF, device="cuda"), ints([length]))
+        want = [row * 0 if length + i >= n else row for i in range(t)]
+        assert torch.equal(out[0, :, 0], torch.stack(want))
+
+
 @pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16), (F32, 64), (F32, 128), (BF, 16)], ids=lambda x: str(x).replace("torch.", ""))
 @pytest.mark.parametrize("src", [BF, F32], ids=["from_bf16", "from_f32"])
 @pytest.mark.parametrize("layers", [0, 3])
