@@ -317,117 +317,96 @@ __global__ __launch_bounds__(256) void block_pick_waves_kernel(BoundP p) {
 // More blocks: a workgroup for the blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the lower block; a bound that
 // is no number comes last.  Order-preserving 64-bit keys; a digit of eight bits at a time from the first bit in which they differ (most keys share sign and exponent,
 // and a histogram of those would be one counter), until the digit that the last chosen one is in holds no more than are wanted.
+// A histogram per digit, all cleared at the start, which every wave adds up by itself: one barrier a digit.
 constexpr int PICK_T = 512, PICK_N = TREE_BLOCKS_MAX / PICK_T;
 __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
-  __shared__ unsigned hist[256];
+  __shared__ __attribute__((aligned(16))) unsigned hist[8][256];
   __shared__ unsigned long long and_s[PICK_T / 64], or_s[PICK_T / 64];
   __shared__ int cnt_s[PICK_N][PICK_T / 64];
-  __shared__ int digit_s, need_s, left_s;
-  __shared__ mask64 ok_s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const TreeP& t = p.t;
+  const size_t row = ((size_t)b * t.kv + hk) * t.T + n;
+  const double* score = p.score + row * p.tiles * 64;
+  double s[PICK_N];                              // (before the length is there; what is behind the complete blocks is not looked at)
+#pragma unroll
+  for (int j = 0; j < PICK_N; ++j) { const int blk = j * PICK_T + tid; s[j] = blk < p.tiles * 64 ? score[blk] : 0.0; }
+  for (int x = tid; x < 8 * 256 / 4; x += PICK_T) ((u32x4*)hist)[x] = u32x4{0, 0, 0, 0};
   int len, there;
   tree_extent(t, b, len, there);
-  if (wave == 0) {
-    mask64 anc; bool ok;
-    tree_ancestors(t, b, there, lane, anc, ok);
-    const mask64 all = __ballot(ok);
-    if (lane == 0) ok_s = all;
-  }
+  mask64 anc; bool ok;
+  tree_ancestors(t, b, there, lane, anc, ok);
+  const bool there_n = __ballot(ok) >> n & 1;
   const int done = len / p.block, lo = min(p.first, done), hi = max(lo, done - p.recent), words = t.words;
-  unsigned* out = p.chosen + (((size_t)b * t.kv + hk) * t.T + n) * words;
-  __syncthreads();
-  const bool there_n = ok_s >> n & 1;
   const int cand = hi - lo, take = there_n ? min(p.top, cand) : 0;
-  const bool everything = take == cand;
-  unsigned long long key[PICK_N];
-  unsigned long long thr = 0;
-  int need = 0;                                  // of the keys that equal thr, so many of the lowest blocks
-  if (!everything && take > 0) {
-    const double* score = p.score + (((size_t)b * t.kv + hk) * t.T + n) * p.tiles * 64;
-    unsigned long long a = ~0ull, o = 0ull;
-#pragma unroll
-    for (int j = 0; j < PICK_N; ++j) {
-      const int blk = j * PICK_T + tid;
-      key[j] = 0;
-      if (blk >= lo && blk < hi) {
-        key[j] = bound_key(score[blk]);
-        a &= key[j]; o |= key[j];
-      }
-    }
-    for (int x = 32; x > 0; x >>= 1) { a &= __shfl_xor(a, x, 64); o |= __shfl_xor(o, x, 64); }
-    if (lane == 0) { and_s[wave] = a; or_s[wave] = o; }
-    __syncthreads();
-    for (int w = 0; w < PICK_T / 64; ++w) { a &= and_s[w]; o |= or_s[w]; }
-    const unsigned long long differ = a ^ o;
-    need = take;
-    int top_bit = differ ? 64 - __clzll((long long)differ) : 0;        // bits from here on up are the same in all
-    thr = top_bit < 64 ? a >> top_bit << top_bit : 0ull;
-    while (top_bit > 0) {
-      const int bits = min(8, top_bit), sh = top_bit - bits;
-      for (int x = tid; x < 256; x += PICK_T) hist[x] = 0;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < PICK_N; ++j) {
-        const int blk = j * PICK_T + tid;
-        if (blk >= lo && blk < hi && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit)) atomicAdd(&hist[(key[j] >> sh) & ((1u << bits) - 1)], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {                           // from the largest digit down: the first at which `need` are reached
-        const int d0 = 255 - 4 * lane;
-        unsigned c[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { c[j] = hist[d0 - j]; mine += c[j]; }
-        unsigned upto = mine;
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) { const unsigned v = __shfl_up(upto, x, 64); if (lane >= x) upto += v; }
-        unsigned before = upto - mine;
-        if (before < (unsigned)need && upto >= (unsigned)need) {
-          int d = d0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (before + c[j] >= (unsigned)need) { d = d0 - j; left_s = (int)c[j]; break; }
-            before += c[j];
-          }
-          digit_s = d; need_s = need - (int)before;
-        }
-      }
-      __syncthreads();
-      thr |= (unsigned long long)digit_s << sh;
-      need = need_s;
-      top_bit = sh;
-      const bool all_of_it = left_s == need;
-      __syncthreads();
-      if (all_of_it) break;                      // (thr's lower bits are zero: every key with these upper ones is at least that)
-    }
-    // ties: `need` keys of those whose upper bits are thr's, the lowest blocks
-#pragma unroll
-    for (int j = 0; j < PICK_N; ++j) {
-      const int blk = j * PICK_T + tid;
-      const bool same = blk >= lo && blk < hi && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit);
-      const mask64 m = __ballot(same);
-      if (lane == 0) cnt_s[j][wave] = __popcll(m);
-    }
-    __syncthreads();
-    int before = 0;
+  unsigned* out = p.chosen + row * words;
+  unsigned chosen = take == cand ? ~0u : 0u;     // bit j: block j PICK_T + tid, if it is a candidate
+  if (take > 0 && take < cand) {
+    unsigned long long key[PICK_N], a = ~0ull, o = 0ull;
 #pragma unroll
     for (int j = 0; j < PICK_N; ++j) {
       const int blk = j * PICK_T + tid;
       const bool in = blk >= lo && blk < hi;
-      const bool same = in && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit);
-      const bool above = in && top_bit < 64 && key[j] >> top_bit > thr >> top_bit;
-      int at = before;
-      for (int w = 0; w < PICK_T / 64; ++w) { if (w < wave) at += cnt_s[j][w]; before += cnt_s[j][w]; }
-      const mask64 m = __ballot(same);
-      const int mine = at + __popcll(m & ((1ull << lane) - 1));
-      key[j] = above || (same && mine < need);   // (from here on: whether it is chosen)
+      key[j] = in ? bound_key(s[j]) : 0ull;      // (0: no candidate's)
+      if (in) { a &= key[j]; o |= key[j]; }
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) { a &= __shfl_xor(a, x, 64); o |= __shfl_xor(o, x, 64); }
+    if (lane == 0) { and_s[wave] = a; or_s[wave] = o; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < PICK_T / 64; ++w) { a &= and_s[w]; o |= or_s[w]; }
+    const unsigned long long differ = a ^ o;
+    int need = take;                             // of the keys whose upper bits are thr's, so many are chosen
+    int top_bit = differ ? 64 - __clzll((long long)differ) : 0;        // bits from here on up are the same in all
+    unsigned long long thr = top_bit < 64 ? a >> top_bit << top_bit : 0ull;
+    bool whole = false;                          // all of those
+    for (int level = 0; top_bit > 0 && !whole; ++level) {
+      const int bits = min(8, top_bit), sh = top_bit - bits;
+#pragma unroll
+      for (int j = 0; j < PICK_N; ++j)
+        if (key[j] && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit)) atomicAdd(&hist[level][(key[j] >> sh) & ((1u << bits) - 1)], 1u);
+      __syncthreads();
+      const u32x4 c = *(const u32x4*)&hist[level][252 - 4 * lane];     // from the largest digit down: the first at which `need` are reached
+      const unsigned mine = c[0] + c[1] + c[2] + c[3];
+      unsigned upto = mine;
+#pragma unroll
+      for (int x = 1; x < 64; x <<= 1) { const unsigned v = __shfl_up(upto, x, 64); if (lane >= x) upto += v; }
+      unsigned before = upto - mine;
+      const int src = __ffsll((long long)__ballot(upto >= (unsigned)need)) - 1;
+      int digit = 255 - 4 * lane;
+      unsigned left = c[3];
+      if (before + left < (unsigned)need) { before += left; left = c[2]; --digit; }
+      if (before + left < (unsigned)need) { before += left; left = c[1]; --digit; }
+      if (before + left < (unsigned)need) { before += left; left = c[0]; --digit; }
+      thr |= (unsigned long long)__builtin_amdgcn_readlane(digit, src) << sh;
+      need -= __builtin_amdgcn_readlane((int)before, src);
+      top_bit = sh;
+      whole = __builtin_amdgcn_readlane((int)left, src) == need;
+    }
+    if (whole) {                                 // (thr's lower bits are zero)
+#pragma unroll
+      for (int j = 0; j < PICK_N; ++j) chosen |= (unsigned)(key[j] >= thr) << j;
+    } else {                                     // ties, of all bits: the lowest blocks
+#pragma unroll
+      for (int j = 0; j < PICK_N; ++j) {
+        const mask64 m = __ballot(key[j] == thr);
+        if (lane == 0) cnt_s[j][wave] = __popcll(m);
+      }
+      __syncthreads();
+      int before = 0;
+#pragma unroll
+      for (int j = 0; j < PICK_N; ++j) {
+        const mask64 m = __ballot(key[j] == thr);
+        int at = before + __popcll(m & ((1ull << lane) - 1));
+        for (int w = 0; w < PICK_T / 64; ++w) { const int c = cnt_s[j][w]; if (w < wave) at += c; before += c; }
+        chosen |= (unsigned)(key[j] > thr || (key[j] == thr && at < need)) << j;
+      }
     }
   }
 #pragma unroll
   for (int j = 0; j < PICK_N; ++j) {
     const int blk = j * PICK_T + tid;
-    const bool mid = blk >= lo && blk < hi && (everything || (take > 0 && key[j]));
-    const bool pick = there_n && blk < done && (blk < lo || blk >= hi || mid);
+    const bool pick = there_n && blk < done && (blk < lo || blk >= hi || (chosen >> j & 1));
     const mask64 m = __ballot(pick);
     const int w = (j * PICK_T + wave * 64) / 32;
     if (lane < 2 && w + lane < words) out[w + lane] = (unsigned)(m >> (32 * lane));
