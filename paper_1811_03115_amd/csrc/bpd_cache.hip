@@ -111,10 +111,10 @@ void choose_blocks(const bpd_cache& c, const BoundP& bp, hipStream_t s) {
   else if (D == 64) hipLaunchKernelGGL((block_bounds_kernel<float, 64, false>), grid, dim3(256), 0, s, bp);
   else hipLaunchKernelGGL((block_bounds_kernel<float, 128, false>), grid, dim3(256), 0, s, bp);
   if (bp.t.T == 0) return;
-  const dim3 waves((bp.t.T + 3) / 4, bp.t.kv, bp.t.B);
-  if (bp.tiles <= 2) hipLaunchKernelGGL(block_pick_waves_kernel<2>, waves, dim3(256), 0, s, bp);
-  else if (bp.tiles <= 8) hipLaunchKernelGGL(block_pick_waves_kernel<8>, waves, dim3(256), 0, s, bp);
-  else hipLaunchKernelGGL(block_pick_kernel, dim3(bp.t.T, bp.t.kv, bp.t.B), dim3(PICK_T), 0, s, bp);
+  const dim3 nodes(bp.t.T, bp.t.kv, bp.t.B);
+  if (bp.tiles <= 2) hipLaunchKernelGGL((block_pick_kernel<128, 1>), nodes, dim3(128), 0, s, bp);
+  else if (bp.tiles <= 8) hipLaunchKernelGGL((block_pick_kernel<512, 1>), nodes, dim3(512), 0, s, bp);
+  else hipLaunchKernelGGL((block_pick_kernel<512, TREE_BLOCKS_MAX / 512>), nodes, dim3(512), 0, s, bp);
 }
 // What the blocks of a call are, and where their bounds and bits go
 BoundP bound_args(TreeP& p, const bpd_cache& c, const bpd_blocks& blocks, unsigned* chosen, double* score) {

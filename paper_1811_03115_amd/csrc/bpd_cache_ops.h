@@ -252,85 +252,24 @@ __device__ __forceinline__ unsigned long long bound_key(double score) {
   const unsigned long long u = (unsigned long long)__double_as_longlong(s);
   return s != s ? 1ull : (u >> 63 ? ~u : u | 1ull << 63);
 }
-// Up to 64 N blocks: a wave per (node, key head, sequence), N bounds a lane, all in registers: the largest threshold that `take` keys reach is found bit by bit from the first bit
-// in which they differ, each bit a count of ballots, until exactly as many reach it.  No LDS and no barriers.  (94 blocks: 11.3 us with the digits below)
-template <int N>
-__global__ __launch_bounds__(256) void block_pick_waves_kernel(BoundP p) {
-  const TreeP& t = p.t;
-  const int lane = threadIdx.x & 63, n = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), hk = blockIdx.y, b = blockIdx.z;
-  if (n >= t.T) return;
-  const size_t row = ((size_t)b * t.kv + hk) * t.T + n;
-  const double* score = p.score + row * p.tiles * 64;
-  double s[N];
-#pragma unroll
-  for (int j = 0; j < N; ++j) s[j] = j < p.tiles ? score[64 * j + lane] : 0.0;
-  int len, there;
-  tree_extent(t, b, len, there);
-  mask64 anc; bool ok;
-  tree_ancestors(t, b, there, lane, anc, ok);
-  const bool there_n = __ballot(ok) >> n & 1;
-  const int done = len / p.block, lo = min(p.first, done), hi = max(lo, done - p.recent), cand = hi - lo, take = min(p.top, cand);
-  unsigned long long key[N], a = ~0ull, o = 0ull;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int blk = 64 * j + lane;
-    const bool in = blk >= lo && blk < hi;
-    key[j] = in ? bound_key(s[j]) : 0ull;        // (0: no candidate's)
-    if (in) { a &= key[j]; o |= key[j]; }
-  }
-  // chosen: keys of at least thr, and the lowest `ties` blocks whose key is `tie`
-  unsigned long long thr = 1, tie = 0;
-  int ties = 0;
-  if (take == 0) thr = ~0ull;                    // (no bound has that key: it would be a NaN)
-  else if (take < cand) {
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) { a &= __shfl_xor(a, x, 64); o |= __shfl_xor(o, x, 64); }
-    const unsigned long long differ = a ^ o;
-    int bit = differ ? 63 - __clzll((long long)differ) : -1;
-    thr = bit < 0 ? a : (bit == 63 ? 0ull : a >> (bit + 1) << (bit + 1));
-    int above = 0;                               // keys over the final threshold's bits so far
-    bool exact = false;
-    for (; bit >= 0 && !exact; --bit) {
-      const unsigned long long c = thr | 1ull << bit;
-      int cnt = 0;
-#pragma unroll
-      for (int j = 0; j < N; ++j) cnt += __popcll(__ballot(key[j] >= c));
-      if (cnt >= take) { thr = c; exact = cnt == take; } else above = cnt;
-    }
-    if (!exact) { tie = thr; ties = take - above; thr = thr + 1; }       // more keys equal the threshold than are wanted
-  }
-  unsigned* out = p.chosen + row * t.words;
-  int before = 0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int blk = 64 * j + lane;
-    const bool in = blk >= lo && blk < hi, same = in && ties && key[j] == tie;
-    const mask64 m = __ballot(same);
-    const bool mine = same && before + __popcll(m & ((1ull << lane) - 1)) < ties;
-    before += __popcll(m);
-    const bool pick = there_n && blk < done && (!in || mine || key[j] >= thr);
-    const mask64 bits = __ballot(pick);
-    if (lane < 2 && 2 * j + lane < t.words) out[2 * j + lane] = (unsigned)(bits >> (32 * lane));
-  }
-}
-
-// More blocks: a workgroup for the blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the lower block; a bound that
-// is no number comes last.  Order-preserving 64-bit keys; a digit of eight bits at a time from the first bit in which they differ (most keys share sign and exponent,
-// and a histogram of those would be one counter), until the digit that the last chosen one is in holds no more than are wanted.
-// A histogram per digit, all cleared at the start, which every wave adds up by itself: one barrier a digit.
-constexpr int PICK_T = 512, PICK_N = TREE_BLOCKS_MAX / PICK_T;
-__global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
+// A workgroup of T threads for the up to T N blocks of one (node, key head, sequence): the first and the last ones, and of the others the `top` with the largest bounds, ties to the
+// lower block; a bound that is no number comes last.  Order-preserving 64-bit keys, in registers; a digit of eight bits at a time from the first bit in which they differ (most keys share
+// sign and exponent, and a histogram of those would be one counter), until the digit that the last chosen one is in holds no more than are wanted.  A histogram per digit,
+// all cleared at the start, which every wave adds up by itself: one barrier a digit.  (Two or three digits mostly: 94 blocks 5.0 us, 1875 5.8, of which a launch is 2.  Bit by bit with ballots, one wave: 94
+// blocks 5.1; eight waves, a barrier a bit: 1875 blocks 9.2.)
+template <int T, int N>
+__global__ __launch_bounds__(T) void block_pick_kernel(BoundP p) {
   __shared__ __attribute__((aligned(16))) unsigned hist[8][256];
-  __shared__ unsigned long long and_s[PICK_T / 64], or_s[PICK_T / 64];
-  __shared__ int cnt_s[PICK_N][PICK_T / 64];
+  __shared__ unsigned long long and_s[T / 64], or_s[T / 64];
+  __shared__ int cnt_s[N][T / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const TreeP& t = p.t;
   const size_t row = ((size_t)b * t.kv + hk) * t.T + n;
   const double* score = p.score + row * p.tiles * 64;
-  double s[PICK_N];                              // (before the length is there; what is behind the complete blocks is not looked at)
+  double s[N];                              // (before the length is there; what is behind the complete blocks is not looked at)
 #pragma unroll
-  for (int j = 0; j < PICK_N; ++j) { const int blk = j * PICK_T + tid; s[j] = blk < p.tiles * 64 ? score[blk] : 0.0; }
-  for (int x = tid; x < 8 * 256 / 4; x += PICK_T) ((u32x4*)hist)[x] = u32x4{0, 0, 0, 0};
+  for (int j = 0; j < N; ++j) { const int blk = j * T + tid; s[j] = blk < p.tiles * 64 ? score[blk] : 0.0; }
+  for (int x = tid; x < 8 * 256 / 4; x += T) ((u32x4*)hist)[x] = u32x4{0, 0, 0, 0};
   int len, there;
   tree_extent(t, b, len, there);
   mask64 anc; bool ok;
@@ -339,12 +278,12 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
   const int done = len / p.block, lo = min(p.first, done), hi = max(lo, done - p.recent), words = t.words;
   const int cand = hi - lo, take = there_n ? min(p.top, cand) : 0;
   unsigned* out = p.chosen + row * words;
-  unsigned chosen = take == cand ? ~0u : 0u;     // bit j: block j PICK_T + tid, if it is a candidate
+  unsigned chosen = take == cand ? ~0u : 0u;     // bit j: block j T + tid, if it is a candidate
   if (take > 0 && take < cand) {
-    unsigned long long key[PICK_N], a = ~0ull, o = 0ull;
+    unsigned long long key[N], a = ~0ull, o = 0ull;
 #pragma unroll
-    for (int j = 0; j < PICK_N; ++j) {
-      const int blk = j * PICK_T + tid;
+    for (int j = 0; j < N; ++j) {
+      const int blk = j * T + tid;
       const bool in = blk >= lo && blk < hi;
       key[j] = in ? bound_key(s[j]) : 0ull;      // (0: no candidate's)
       if (in) { a &= key[j]; o |= key[j]; }
@@ -354,7 +293,7 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
     if (lane == 0) { and_s[wave] = a; or_s[wave] = o; }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < PICK_T / 64; ++w) { a &= and_s[w]; o |= or_s[w]; }
+    for (int w = 0; w < T / 64; ++w) { a &= and_s[w]; o |= or_s[w]; }
     const unsigned long long differ = a ^ o;
     int need = take;                             // of the keys whose upper bits are thr's, so many are chosen
     int top_bit = differ ? 64 - __clzll((long long)differ) : 0;        // bits from here on up are the same in all
@@ -363,7 +302,7 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
     for (int level = 0; top_bit > 0 && !whole; ++level) {
       const int bits = min(8, top_bit), sh = top_bit - bits;
 #pragma unroll
-      for (int j = 0; j < PICK_N; ++j)
+      for (int j = 0; j < N; ++j)
         if (key[j] && (top_bit >= 64 || key[j] >> top_bit == thr >> top_bit)) atomicAdd(&hist[level][(key[j] >> sh) & ((1u << bits) - 1)], 1u);
       __syncthreads();
       const u32x4 c = *(const u32x4*)&hist[level][252 - 4 * lane];     // from the largest digit down: the first at which `need` are reached
@@ -385,30 +324,30 @@ __global__ __launch_bounds__(PICK_T) void block_pick_kernel(BoundP p) {
     }
     if (whole) {                                 // (thr's lower bits are zero)
 #pragma unroll
-      for (int j = 0; j < PICK_N; ++j) chosen |= (unsigned)(key[j] >= thr) << j;
+      for (int j = 0; j < N; ++j) chosen |= (unsigned)(key[j] >= thr) << j;
     } else {                                     // ties, of all bits: the lowest blocks
 #pragma unroll
-      for (int j = 0; j < PICK_N; ++j) {
+      for (int j = 0; j < N; ++j) {
         const mask64 m = __ballot(key[j] == thr);
         if (lane == 0) cnt_s[j][wave] = __popcll(m);
       }
       __syncthreads();
       int before = 0;
 #pragma unroll
-      for (int j = 0; j < PICK_N; ++j) {
+      for (int j = 0; j < N; ++j) {
         const mask64 m = __ballot(key[j] == thr);
         int at = before + __popcll(m & ((1ull << lane) - 1));
-        for (int w = 0; w < PICK_T / 64; ++w) { const int c = cnt_s[j][w]; if (w < wave) at += c; before += c; }
+        for (int w = 0; w < T / 64; ++w) { const int c = cnt_s[j][w]; if (w < wave) at += c; before += c; }
         chosen |= (unsigned)(key[j] > thr || (key[j] == thr && at < need)) << j;
       }
     }
   }
 #pragma unroll
-  for (int j = 0; j < PICK_N; ++j) {
-    const int blk = j * PICK_T + tid;
+  for (int j = 0; j < N; ++j) {
+    const int blk = j * T + tid;
     const bool pick = there_n && blk < done && (blk < lo || blk >= hi || (chosen >> j & 1));
     const mask64 m = __ballot(pick);
-    const int w = (j * PICK_T + wave * 64) / 32;
+    const int w = (j * T + wave * 64) / 32;
     if (lane < 2 && w + lane < words) out[w + lane] = (unsigned)(m >> (32 * lane));
   }
 }

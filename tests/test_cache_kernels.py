@@ -33,6 +33,6 @@ def test_no_cache_kernel_uses_scratch(tmp_path):
         if m:
             found[cur] = int(m.group(1))
     for kernel in ("tree_attention_kernel", "tree_attention_rows_kernel", "tree_rows_kernel", "tree_join_kernel", "store_groups_kernel", "store_rows_kernel",
-                   "block_bounds_kernel", "block_pick_waves_kernel", "block_pick_kernel", "tree_accept_kernel", "tree_move_kernel"):
+                   "block_bounds_kernel", "block_pick_kernel", "tree_accept_kernel", "tree_move_kernel"):
         assert any(kernel in name for name in found), f"{kernel} not found"
     assert not {n: s for n, s in found.items() if s > 0}
