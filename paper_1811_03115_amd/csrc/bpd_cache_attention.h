@@ -114,6 +114,10 @@ __device__ __forceinline__ void tree_store4(const TreeP& p, int b, int node, int
   }
 }
 // Eight elements of a query (c % 8 == 0) in fp32
+__device__ __forceinline__ float tree_q1(const TreeP& p, int b, int node, int h, int c) {
+  const long at = (long)b * p.q_seq + (long)node * p.q_row + (long)h * p.q_head + c;
+  return p.q_f32 ? ((const float*)p.q)[at] : bf2f(((const bf16_t*)p.q)[at]);
+}
 __device__ __forceinline__ void tree_q8(const TreeP& p, int b, int node, int h, int c, float (&v)[8]) {
   const long at = (long)b * p.q_seq + (long)node * p.q_row + (long)h * p.q_head + c;
   if (p.q_f32) {

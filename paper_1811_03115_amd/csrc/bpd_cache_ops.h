@@ -142,6 +142,20 @@ template <> struct Eight<float> {
   }
 };
 typedef double f64x4 __attribute__((ext_vector_type(4)));
+// The bound of one (node, block), term by term: sum is where the block's summary begins.  (No key but NaN in a dimension: no number.)
+template <typename S, int D>
+__device__ double block_bound(const TreeP& t, int b, int n, int hk, const S* sum) {
+  double bound = 0.0;
+  for (int c = 0; c < D; ++c) {
+    const S* at = sum + (size_t)(c / 8) * 512 + c % 8;
+    const double mn = to_f<S>(at[0]), mx = to_f<S>(at[(size_t)(D / 8) * 512]);
+    for (int g = 0; g < t.G; ++g) {
+      const double v = tree_q1(t, b, n, hk * t.G + g, c), x = v * mn, y = v * mx;
+      bound += mn > mx ? (double)NAN : (x != x ? x : (y != y || y > x ? y : x));
+    }
+  }
+  return bound;
+}
 // Upper bound of a group's scores in a block, summed over its G heads:  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
 // the heads are added first and cost nothing, and what is left is a product of 16 nodes with 64 blocks over 2 D.  In 64 bits, on v_mfma_f64_16x16x4_f64: products of bf16 numbers and
 // their sums are then as good as exact, and which blocks are chosen does not depend on an order of summation.  (On the vector units the nodes' sums, the same for all lanes, come out
@@ -239,6 +253,10 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
     }
   }
   acc += odd;
+  // (a part that is zero times an infinite key is no number: then the sum as it is defined)
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (acc[i] != acc[i] && 4 * i + q < nn && blk0 + 16 * wave + c < done) acc[i] = block_bound<S, D>(t, b, n0 + 4 * i + q, hk, sum + (16 * wave + c) * 8);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {                  // node 4 i + q, block c of the wave's
     const int n = 4 * i + q;

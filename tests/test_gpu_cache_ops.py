@@ -371,6 +371,34 @@ def test_sparse_many_blocks():
         ref.check(got, want, off)
 
 
+@pytest.mark.parametrize("blocks", [1, 64, 65, 128, 129, 500, 512, 513, 1600])
+def test_sparse_which_blocks(blocks):
+    """Which blocks are chosen, in one tile and in many: bounds of both signs, with many ties, infinite ones and ones that are no number."""
+    rng = np.random.default_rng(blocks)
+    d, block, kv, b = 64, 32, 2, 2
+    cap = blocks * block
+    k = torch.from_numpy(rng.integers(-2, 3, (b, blocks, 1, kv, d)).astype(np.float32)).repeat(1, 1, block, 1, 1).reshape(b, cap, kv, d)
+    k[:, :, :, 2:] *= 0.125
+    k[0, ::max(1, cap // 7), 0, 0] = float("inf")
+    k[1, cap // 3:cap // 3 + 40, 1, 1] = float("-inf")
+    k = k.to(BF)
+    v = rows(rng, b, cap, kv, d)
+    q = torch.zeros((b, 4, kv, d))
+    q[:, 0, :, :2] = torch.tensor([1.0, -1.0])
+    q[:, 1, :, :2] = torch.tensor([-3.0, 2.0])
+    q[:, 2] = rows(rng, b, kv, d, dtype=F32)
+    q = q.to(BF)                                                          # (node 3: bounds of zero, or none)
+    cache = tuple(cuda(x) for x in ref.pack(k, v))
+    parent = np.full((b, 4), -1, np.int32)
+    summ = binding.new_summaries(cache, block)
+    lengths = [max(0, cap - 4), cap // 2]
+    for first, recent, top in ((0, 0, 1), (1, 2, max(1, blocks // 3)), (0, 0, blocks), (2, 1, 0)):
+        what = dict(block=block, first=first, recent=recent, top=top)
+        _, _, picks = ref.attention(q, k, v, lengths, parent, blocks=what)
+        _, chosen = bpd.bpd_sparse_attention(cache, cuda(q), ints(lengths), summ, parent=cuda(parent), **what)
+        assert torch.equal(chosen.cpu(), picks), what
+
+
 # ------------------------------------------------------------------------------------------------ accept
 
 @pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16), (F32, 128), (BF, 16), (None, 0)], ids=lambda x: str(x).replace("torch.", ""))
