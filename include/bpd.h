@@ -253,8 +253,8 @@ int bpd_set_local_attention(bpd_ctx* ctx, int query_block, int memory_len);
 /* Decoder self-attention by chosen blocks (bpd_sparse_attention below): every row of a step sees, of the committed prefix, the first
  * `first` and the last `recent` complete blocks of `block` rows (32, 64 or 128), the `top` others with the largest bound of its
  * scores per head, and what is behind the last complete block; and the step's own rows as ever.  For very long outputs: eight images with
- * 29 blocks of 32 are faster from some 18000 positions on (23000: 473 us a step with all keys, 410), below that the kernel of all
- * layers that full attention has outweighs the keys left out (2900: 193 us, 322).  block = 0 (the rest is ignored) restores attention to all keys, the default; the setting may change
+ * 29 blocks of 32 are faster from some 16000 positions on (23000: 472 us a step with all keys, 396), below that the kernel of all
+ * layers that full attention has outweighs the keys left out (2900: 194 us, 314).  block = 0 (the rest is ignored) restores attention to all keys, the default; the setting may change
  * between steps, and applies to later bpd_step / bpd_step_tree / bpd_decode / bpd_debug_step_logits calls (whose layers then run kernel by
  * kernel).
  *   buffer [device] caller-owned, 256-byte aligned, bpd_sparse_buffer_bytes(ctx, block), not shared with another context; it must stay

@@ -49,12 +49,18 @@ const char* rows_wrong(const bpd_rows* r) {
 RowsP rows_of(const bpd_rows& r) { return RowsP{r.data, r.dtype == BPD_F32, rows_aligned(r) ? 1 : 0, (long)r.layer, (long)r.seq, (long)r.row, (long)r.head}; }
 
 template <int D, int MT, int NW, bool SPARSE>
-void attend_few(const TreeP& p, hipStream_t s) {
+void attend_waves(const TreeP& p, hipStream_t s) {
   const dim3 grid(p.parts, p.kv);
   if constexpr (MT == 1 || (MT == 2 && D == 64)) {      // (more rows of fp32 queries: attend_groups)
     if (p.q_f32) { hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, true, SPARSE>), grid, dim3(64 * NW), 0, s, p); return; }
   }
   hipLaunchKernelGGL((tree_attention_kernel<D, MT, NW, false, SPARSE>), grid, dim3(64 * NW), 0, s, p);
+}
+template <int D, int MT, bool SPARSE>
+void attend_few(const TreeP& p, hipStream_t s) {
+  // Eight waves where one workgroup has all of the keys (split_of()), they are more than four waves' first items, and a CU would have no second workgroup.  (64-wide, 32 rows, 128 pairs, 94 groups
+  // 22.6 us a call, four waves 26.1; 1024 pairs, 5 groups: a step of six layers 709 us, 678.)
+  if (p.nsplit == 1 && p.cap > 128 && (long)p.parts * p.kv <= compute_units()) attend_waves<D, MT, 8, SPARSE>(p, s); else attend_waves<D, MT, 4, SPARSE>(p, s);
 }
 template <int D, bool SPARSE>
 void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
@@ -64,10 +70,10 @@ void attend_groups(const TreeP& p, const TreePlan& plan, hipStream_t s) {
     else if (plan.mt == 1) hipLaunchKernelGGL((tree_attention_rows_kernel<D, 1, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
     else hipLaunchKernelGGL((tree_attention_rows_kernel<D, 2, 4, false, SPARSE>), dim3(p.parts * plan.blocks, p.kv), dim3(256), 0, s, p);
   } else if constexpr (D == 64) {
-    if (plan.mt == 1) attend_few<D, 1, 4, SPARSE>(p, s);
-    else if (plan.mt == 2) attend_few<D, 2, 4, SPARSE>(p, s);
-    else attend_few<D, 3, 4, SPARSE>(p, s);
-  } else attend_few<D, 1, 4, SPARSE>(p, s);
+    if (plan.mt == 1) attend_few<D, 1, SPARSE>(p, s);
+    else if (plan.mt == 2) attend_few<D, 2, SPARSE>(p, s);
+    else attend_few<D, 3, SPARSE>(p, s);
+  } else attend_few<D, 1, SPARSE>(p, s);
 }
 template <int D>
 void join(const TreeP& p, hipStream_t s) {

@@ -36,17 +36,27 @@ inline size_t summaries_elements(const bpd_cache& c, int block) {
   return (size_t)c.max_batch * c.n_kv_heads * tiles * 2 * c.head_dim * 64;
 }
 
-struct TreePlan { bool rows; int mt, blocks, nsplit; size_t chosen_at, score_at, bytes; };
+struct TreePlan { bool rows; int mt, wide, blocks, nsplit; size_t chosen_at, score_at, bytes; };
 // Parts that `groups` of 32 keys are split into, for as many (sequence, key head, row block)s as there are: the fewest rounds of as many workgroups as the chip has room for (a CU's
 // registers: four of fp32 rows, three of 64 rows that share 128-wide keys, otherwise two) times what a workgroup takes, in units of an item: its items (one in four where the
-// waves split them) and five for its beginning and end; four more for joining parts.  (52 x 4 row blocks over 46 groups: three parts, 624 workgroups, 74 us; two 51.
-// 64 pairs, 95 groups: one part 29 us, four 21, eight 17.)
+// waves split them) and five for its beginning and end; four more for joining parts.  (52 x 4 row blocks over 46 groups: three parts, 624 workgroups, 74 us; two 51.)
+// Where every wave takes items of its own, one workgroup of eight waves for all of them is the other way, without the second launch.  Its time in us: an item is 8 KiB of
+// 64-wide keys and values, 5.2 TB/s for all and some 100 GB/s for one CU's (tiles of 16 rows: that many times as much); of the two the longer one and a tenth of the other, and
+// 5.5 for the launch.  In parts: the first, the waves' own items at 0.5, the launch, and 3 for joining; and never less than the 14.6 that the host takes for two launches (one: 11.6).
+// Not if it takes longer than that and the cache is one whose parts go by length (attend()): one sequence alone may be long.
+// (64-wide, 64 pairs, 94 groups: one part 14.3 us a call, eight 16.2; 8 pairs, 94 groups 12.4, 14.5; 188 groups 17.5, 14.8.  128-wide, 128 pairs, 31 groups: 15.5, 19.2; 32 pairs, 94 groups:
+// 22, 16.5.)
 inline int split_of(const TreePlan& p, long pairs, long groups, bool grouped, int cus) {
   const long room = (long)(!grouped ? 4 : (p.rows && p.mt == 1 ? 3 : 2)) * cus, step = p.rows ? 1 : 4;
   long best = 1, least = 0;
   for (long n = 1; n <= 64 && (n == 1 || n * 4 <= groups); ++n) {
     const long cost = (pairs * n + room - 1) / room * ((groups + n * step - 1) / (n * step) + 5) + (n > 1 ? 4 : 0);
     if (n == 1 || cost < least) { best = n; least = cost; }
+  }
+  if (best > 1 && grouped && !p.rows) {
+    const double hbm = 0.0016 * p.wide * pairs * groups, cu = 0.08 * p.wide * p.mt * ((pairs + cus - 1) / cus) * groups;
+    const double one = 5.5 + (hbm > cu ? hbm + 0.1 * cu : cu + 0.1 * hbm), parts = 5.5 + hbm + 0.5 * ((groups + 4 * best - 1) / (4 * best)) + 3;
+    if (one <= 14.6 || (one <= parts && groups < 128)) best = 1;
   }
   return (int)best;
 }
@@ -58,6 +68,7 @@ inline TreePlan plan_attention(const bpd_cache& c, int B, int T, int heads, int 
   const bool grouped = cache_grouped(c);
   p.rows = grouped && R > (c.head_dim == 64 ? 48 : 16);        // (more tiles than that in one wave's registers: spills)
   p.mt = p.rows ? (R > 64 ? 2 : 1) : (grouped ? (R + 15) / 16 : 1);
+  p.wide = c.head_dim / 64;
   const int per = p.rows ? 64 * p.mt : (grouped ? 48 : 16);
   p.blocks = (R + per - 1) / per;
   p.nsplit = split_of(p, (long)B * c.n_kv_heads * p.blocks, (c.capacity + 31) / 32, grouped, cus);
