@@ -39,7 +39,9 @@ inline size_t summaries_elements(const bpd_cache& c, int block) {
 struct TreePlan { bool rows; int mt, wide, blocks, nsplit; size_t chosen_at, score_at, bytes; };
 // Parts that `groups` of 32 keys are split into, for as many (sequence, key head, row block)s as there are: the fewest rounds of as many workgroups as the chip has room for (a CU's
 // registers: four of fp32 rows, three of 64 rows that share 128-wide keys, otherwise two) times what a workgroup takes, in units of an item: its items (one in four where the
-// waves split them) and five for its beginning and end; four more for joining parts.  (52 x 4 row blocks over 46 groups: three parts, 624 workgroups, 74 us; two 51.)
+// waves split them) and five for its beginning and end; and for joining parts four more, or, of rows that share keys, 4 us and what writing and reading them takes, by an
+// item's 0.24 us for each 16 rows of a wave and as much for each 64 dimensions.  (52 x 4 row blocks over 46 groups: three parts, 624 workgroups, 74 us; two 51.  32 pairs of 512 rows, 10 groups:
+// 128-wide one part 25.5 us, three 33.9; 64-wide 20.1, 29.6.)
 // Where every wave takes items of its own, one workgroup of eight waves for all of them is the other way, without the second launch.  Its time in us: an item is 8 KiB of
 // 64-wide keys and values, 5.2 TB/s for all and some 100 GB/s for one CU's (tiles of 16 rows: that many times as much); of the two the longer one and a tenth of the other, and
 // 5.5 for the launch.  In parts: the first, the waves' own items at 0.5, the launch, and 3 for joining; and never less than the 14.6 that the host takes for two launches (one: 11.6).
@@ -48,9 +50,11 @@ struct TreePlan { bool rows; int mt, wide, blocks, nsplit; size_t chosen_at, sco
 // 22, 16.5.)
 inline int split_of(const TreePlan& p, long pairs, long groups, bool grouped, int cus) {
   const long room = (long)(!grouped ? 4 : (p.rows && p.mt == 1 ? 3 : 2)) * cus, step = p.rows ? 1 : 4;
-  long best = 1, least = 0;
+  long best = 1;
+  double least = 0;
   for (long n = 1; n <= 64 && (n == 1 || n * 4 <= groups); ++n) {
-    const long cost = (pairs * n + room - 1) / room * ((groups + n * step - 1) / (n * step) + 5) + (n > 1 ? 4 : 0);
+    const double join = n == 1 ? 0 : (p.rows ? (4 + 0.0063 * pairs * n * p.mt * p.wide) / (0.24 * (p.mt + p.wide)) : 4);
+    const double cost = (double)((pairs * n + room - 1) / room * ((groups + n * step - 1) / (n * step) + 5)) + join;
     if (n == 1 || cost < least) { best = n; least = cost; }
   }
   if (best > 1 && grouped && !p.rows) {
