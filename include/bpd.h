@@ -259,7 +259,8 @@ int bpd_set_local_attention(bpd_ctx* ctx, int query_block, int memory_len);
  * kernel).
  *   buffer [device] caller-owned, 256-byte aligned, bpd_sparse_buffer_bytes(ctx, block), not shared with another context; it must stay
  *       valid as long as the setting does (and as long as steps captured under it are replayed).  Summaries of what is committed
- *       already are made here (enqueued): call it again before replaying steps captured under it if others have been replayed or run since.
+ *       already are made here (enqueued): call it again, with the same buffer, before replaying steps captured under it if others have been replayed or
+ *       run since.
  * Errors: BPD_E_ARG (also with local attention set), BPD_E_CAPACITY (buffer; more than BPD_BLOCKS_MAX blocks). */
 int bpd_set_sparse_attention(bpd_ctx* ctx, int block, int first, int recent, int top, void* buffer, size_t bytes);
 size_t bpd_sparse_buffer_bytes(const bpd_ctx* ctx, int block);   /* 0: no such block */

@@ -328,6 +328,7 @@ class Context:
             raise BpdError(rc, "bpd_create failed")
         self.h = handle
         self.B = 0
+        self.sparse_buffers = {}                 # by rows of a block (bpd_set_sparse_attention)
 
     # -- helpers
     def _check(self, rc: int):
@@ -396,13 +397,17 @@ class Context:
         return self.L.bpd_sparse_buffer_bytes(self.h, block)
 
     def bpd_set_sparse_attention(self, block: int, first: int = 1, recent: int = 2, top: int = 8):
-        """block 0: all keys again.  The context keeps the buffer."""
+        """block 0: all keys again.  The context keeps a buffer for each size of blocks as long as it lives: steps that have been captured under a setting have its
+        address, also behind a setting of no blocks, and find the summaries that a later call of this makes."""
         torch = self.torch
         nbytes = self.bpd_sparse_buffer_bytes(block) if block else 0
-        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
-            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device) if nbytes else None
+        buf = self.sparse_buffers.get(block)
+        if buf is None and nbytes:
+            with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+                buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         self._check(self.L.bpd_set_sparse_attention(self.h, block, first, recent, top, (buf.data_ptr() + 255) // 256 * 256 if buf is not None else None, nbytes))
-        self.sparse_buffer = buf
+        if buf is not None:
+            self.sparse_buffers[block] = buf
 
     def bpd_set_acceptance(self, distance_eps: int = 0, min_block: int = 1):
         self._check(self.L.bpd_set_acceptance(self.h, distance_eps, min_block))
