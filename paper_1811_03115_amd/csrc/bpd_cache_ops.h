@@ -242,8 +242,10 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
   if (f1 > f0) load();
   __syncthreads();
   const bool known = blk0 + 16 * wave + c < done;
-  auto finish = [&](int n, double bound) {       // (a part that is zero times an infinite key is no number: then the sum as it is defined)
-    if (bound != bound && known) bound = block_bound<S, D>(t, b, n0 + n, hk, sum + (16 * wave + c) * 8);
+  // (Not finite: the sum as it is defined.  A part that is zero times an infinite key is no number, and heads that have been added first hide such a part of one of them, or make -inf
+  // of a dimension without a key.)
+  auto finish = [&](int n, double bound) {
+    if (!(fabs(bound) < (double)INFINITY) && known) bound = block_bound<S, D>(t, b, n0 + n, hk, sum + (16 * wave + c) * 8);
     p.score[((((size_t)b * t.kv + hk) * t.T + n0 + n) * p.tiles + tile) * 64 + 16 * wave + c] = bound;
   };
   if (nn <= 2) {                                 // (most of the product would be of nodes that are not there: one node, 1875 blocks of 128 dimensions 7.5 us instead of 8.9)

@@ -1,0 +1,88 @@
+"""The cache operators where keys, queries and scales are not the usual ones."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as ref
+from paper_1811_03115_amd import binding
+from paper_1811_03115_amd.binding import Context as bpd
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+INF, NAN = float("inf"), float("nan")
+
+
+def rows(rng, *shape, dtype=BF):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(dtype)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def packed(k, v):
+    return tuple(x.cuda() for x in ref.pack(k, v))
+
+
+# ------------------------------------------------------------------------------------------------ bounds that are not finite
+
+def bound(q, block):
+    """Of the heads q [G, D] and a block's keys [rows, D], as bpd.h has it: NaN keys aside, no number where a dimension has no key but those."""
+    none = torch.isnan(block)
+    lo, hi = torch.where(none, torch.full_like(block, INF), block).amin(0), torch.where(none, torch.full_like(block, -INF), block).amax(0)
+    one = torch.maximum(q * lo, q * hi)
+    return float(torch.where(none.all(0), torch.full_like(one, NAN), one).sum())
+
+
+def chosen_of(q, k, n, block, first, recent, top):
+    done = n // block
+    always = [j for j in range(done) if j < first or j >= done - recent]
+    rest = [(bound(q, k[j * block:(j + 1) * block]), j) for j in range(done) if j not in always]
+    rest.sort(key=lambda x: (math.isnan(x[0]), -x[0] if not math.isnan(x[0]) else 0, x[1]))
+    return sorted(always + [j for _, j in rest[:top]])
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16)], ids=lambda x: str(x).replace("torch.", ""))
+@pytest.mark.parametrize("g", [1, 2, 3])
+@pytest.mark.parametrize("blocks,t", [(9, 4), (9, 1), (150, 5), (530, 2)])
+def test_which_blocks_with_heads_that_share_keys(dtype, d, g, blocks, t):
+    """Infinite keys beside heads of zero, dimensions of nothing but NaN beside heads of both signs: what the sum is defined to be ranks the block, not what the heads add up to.
+    (Small whole numbers: sums are exact in any order.)"""
+    rng = np.random.default_rng(blocks + 7 * g + d)
+    block, kv = 32, 2
+    cap = (blocks + 1) * block
+    k = torch.from_numpy(rng.integers(-3, 4, (1, cap, kv, d)).astype(np.float32)) * 0.125
+    for j in range(blocks):
+        part = k[0, j * block:(j + 1) * block]
+        kind = int(rng.integers(0, 8))
+        if kind == 0:
+            part[5, :, 0] = INF
+        elif kind == 1:
+            part[:, :, 1] = NAN
+        elif kind == 2:
+            part[9, :, 2] = -INF
+        elif kind == 3:
+            part[3:20, :, 3] = NAN
+        elif kind == 4:
+            part[7, :, 0], part[8, :, 2] = INF, -INF
+    k = k.to(dtype)
+    q = torch.from_numpy(rng.integers(-3, 4, (1, t, kv * g, d)).astype(np.float32))
+    q[0, 0, :, :4] = 0
+    q[0, 0, ::2, :4] = torch.tensor([1.0, 2.0, -1.0, 1.0])               # the other heads of a group: exactly zero there
+    if g > 1:
+        q[0, 0, 1::g, 1] = -2.0
+    if t > 2:
+        q[0, 2] = 0
+    q = q.to(dtype)
+    cache = packed(k, rows(rng, *k.shape, dtype=dtype))
+    n = blocks * block + 3
+    parent = np.full((1, t), -1, np.int32)
+    for first, recent, top in ((0, 0, 1), (0, 0, blocks // 2), (1, 1, 3), (0, 0, blocks - 1)):
+        _, chosen = bpd.bpd_sparse_attention(cache, q.cuda(), ints([n]), binding.new_summaries(cache, block), block=block, first=first, recent=recent, top=top, parent=torch.from_numpy(parent).cuda())
+        got = chosen.cpu().numpy().view(np.uint32)
+        for i in range(t):
+            for h in range(kv):
+                want = chosen_of(q[0, i, h * g:(h + 1) * g].double(), k[0, :, h].double(), n, block, first, recent, top)
+                assert [j for j in range(blocks) if int(got[0, h, i, j // 32]) >> (j % 32) & 1] == want, (first, recent, top, i, h)
