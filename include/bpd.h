@@ -401,8 +401,9 @@ int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows
 /* Which blocks of the prefix bpd_sparse_attention sees.  The prefix is cut in blocks of `block` rows, of which
  * n = length / block are complete.  Seen: the first `first`, the last `recent` of them, and of the others
  * the `top` with the largest bound of the scores in them, for each node and key head:
- *     sum over the group's heads of  sum_c max(q_c min_c, q_c max_c),   min, max over the block's keys (NaN aside),
- * in 64 bits, ties to the lower block, a bound that is NaN last.  Rows behind the last complete block are always seen. */
+ *     sum over the group's heads of  sum_c max(s q_c min_c, s q_c max_c),   min, max over the block's keys (NaN aside),
+ * s the scale's sign (1, -1, or 0: then all bounds are alike), in 64 bits, ties to the lower block, a bound that is NaN last.  Rows behind the last
+ * complete block are always seen. */
 typedef struct {
   int32_t block;           /* 32, 64 or 128 rows                                              */
   int32_t first, recent, top;

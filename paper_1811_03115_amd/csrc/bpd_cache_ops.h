@@ -150,13 +150,13 @@ __device__ double block_bound(const TreeP& t, int b, int n, int hk, const S* sum
     const S* at = sum + (size_t)(c / 8) * 512 + c % 8;
     const double mn = to_f<S>(at[0]), mx = to_f<S>(at[(size_t)(D / 8) * 512]);
     for (int g = 0; g < t.G; ++g) {
-      const double v = tree_q1(t, b, n, hk * t.G + g, c), x = v * mn, y = v * mx;
+      const double v = t.sign * tree_q1(t, b, n, hk * t.G + g, c), x = v * mn, y = v * mx;
       bound += mn > mx ? (double)NAN : (x != x ? x : (y != y || y > x ? y : x));
     }
   }
   return bound;
 }
-// Upper bound of a group's scores in a block, summed over its G heads:  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
+// Upper bound of a group's scores in a block, summed over its G heads (q: with the scale's sign):  sum_g sum_c max(q_gc min_c, q_gc max_c) = sum_c max_c sum_g q+_gc + min_c sum_g q-_gc, so that
 // the heads are added first and cost nothing, and what is left is a product of 16 nodes with 64 blocks over 2 D.  In 64 bits, on v_mfma_f64_16x16x4_f64: products of bf16 numbers and
 // their sums are then as good as exact, and which blocks are chosen does not depend on an order of summation.  (On the vector units the nodes' sums, the same for all lanes, come out
 // of LDS once per block and wave, which bounds it: 7 nodes, 1000 blocks of 128 dimensions in 32 pairs 13.6 us.)
@@ -189,7 +189,10 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundP p) {
         float v[8];
         tree_q8(t, b, n0 + n, hk * t.G + g, 8 * c8, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { pos[j] += (double)(v[j] < 0.f ? 0.f : v[j]); neg[j] += (double)(v[j] > 0.f ? 0.f : v[j]); }      // (one that is no number goes to both)
+        for (int j = 0; j < 8; ++j) {            // (the scale's size changes no order, its sign does; one that is no number goes to both)
+          const float x = v[j] * t.sign;
+          pos[j] += (double)(x < 0.f ? 0.f : x); neg[j] += (double)(x > 0.f ? 0.f : x);
+        }
       }
     }
 #pragma unroll

@@ -86,3 +86,23 @@ def test_which_blocks_with_heads_that_share_keys(dtype, d, g, blocks, t):
             for h in range(kv):
                 want = chosen_of(q[0, i, h * g:(h + 1) * g].double(), k[0, :, h].double(), n, block, first, recent, top)
                 assert [j for j in range(blocks) if int(got[0, h, i, j // 32]) >> (j % 32) & 1] == want, (first, recent, top, i, h)
+
+
+# ------------------------------------------------------------------------------------------------ scales
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16), (F32, 64), (BF, 16)], ids=lambda x: str(x).replace("torch.", ""))
+@pytest.mark.parametrize("kv,g,t,n,cap", [(2, 2, 6, 700, 736), (1, 1, 1, 2500, 2560), (1, 3, 19, 4100, 4160)])
+def test_chosen_blocks_of_other_scales(dtype, d, kv, g, t, n, cap):
+    """The blocks are those with the largest bounds of the SCORES: under a negative scale those of the queries turned round, under none all are alike."""
+    rng = np.random.default_rng(d + t)
+    k, v = rows(rng, 1, cap, kv, d, dtype=dtype), rows(rng, 1, cap, kv, d, dtype=dtype)
+    q = rows(rng, 1, t, kv * g, d, dtype=dtype)
+    parent = np.array([[-1] + [i // 2 for i in range(t - 1)]], np.int32)
+    cache = packed(k, v)
+    what = dict(block=32, first=1, recent=1, top=5)
+    for scale in (-0.3, 0.0, -2.0, 0.3):
+        sign = (scale > 0) - (scale < 0)
+        want, off, picks = ref.attention(q * sign, k, v, [n], parent, scale=abs(scale) or 1.0, blocks=what)
+        got, chosen = bpd.bpd_sparse_attention(cache, q.cuda(), ints([n]), binding.new_summaries(cache, 32), scale=scale, parent=torch.from_numpy(parent).cuda(), **what)
+        assert torch.equal(chosen.cpu(), picks), scale
+        ref.check(got, want, off, what=str(scale))
