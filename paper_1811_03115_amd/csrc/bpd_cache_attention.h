@@ -344,16 +344,21 @@ __device__ __forceinline__ void tree_q_operand(const TreeP& p, int b, int hk, in
   for (int j = 0; j < 8; ++j) v[j] *= p.sign;    // (of the scale: the maximum is that of the products)
   tree_pair(v, hi, lo);
 }
-// A row's result or partial result: dimensions c .. c + 3.  Partial results: [key head][part][row][D], then [key head][part][row] maxima and as many sums
-__device__ __forceinline__ void tree_finish4(const TreeP& p, int D, int b, int hk, int part, int r, int R, int node, int c, float M, float L, const f32x4& o) {
+// What a row's sums make of it.  No weights at all: an absent node's zeros, or (there: all of its scores are -inf) no number, 0 / 0
+__device__ __forceinline__ f32x4 tree_quotient(const f32x4& o, float L, bool there) {
+  const float none = L != L || there ? NAN : 0.f;
+  return L > 0.f ? o * (1.f / L) : f32x4{none, none, none, none};
+}
+// A row's result or partial result: dimensions c .. c + 3; there: its node is not absent.  Partial results: [key head][part][row][D], then [key head][part][row] maxima and as many sums
+// (of a row that is there and has no weights in the part: 1, which the maximum of -inf takes away where another part has some)
+__device__ __forceinline__ void tree_finish4(const TreeP& p, int D, int b, int hk, int part, int r, int R, int node, bool there, int c, float M, float L, const f32x4& o) {
   if (r >= R) return;
   if (p.parts > p.B) {
     const long at = ((long)hk * p.parts + part) * R + r, rows = (long)p.kv * p.parts * R;
     *(f32x4*)(p.part + at * D + c) = o;
-    if (c == 0) { p.part[rows * D + at] = M; p.part[rows * (D + 1) + at] = L; }
+    if (c == 0) { p.part[rows * D + at] = M; p.part[rows * (D + 1) + at] = L == 0.f && there ? 1.f : L; }
   } else {
-    // (an absent node has seen nothing: L = 0)
-    tree_store4(p, b, node, hk * p.G + r - node * p.G, c, L > 0.f ? o * (1.f / L) : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
+    tree_store4(p, b, node, hk * p.G + r - node * p.G, c, tree_quotient(o, L, there));
   }
 }
 
@@ -507,7 +512,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
     __syncthreads();
     for (int x = wave; x < VT; x += NW) {
       const f32x4 o = (o_s[0][x][lane] + o_s[1][x][lane]) + (o_s[2][x][lane] + o_s[3][x][lane]);
-      tree_finish4(p, D, b, hk, at_part, 16 * t + lr, R, node[t], 16 * x + 4 * lq, M[t], L[t], o);
+      tree_finish4(p, D, b, hk, at_part, 16 * t + lr, R, node[t], row_ok[t], 16 * x + 4 * lq, M[t], L[t], o);
     }
     if (t + 1 < MT) __syncthreads();
   }
@@ -618,7 +623,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
   for (int t = 0; t < MT; ++t) {
     const float L = sum_rows(tiles.l[t]);
 #pragma unroll
-    for (int x = 0; x < VT; ++x) tree_finish4(p, D, b, hk, at_part, r0 + 16 * t + lr, R, node[t], 16 * x + 4 * lq, tiles.m[t], L, tiles.acc[t][x]);
+    for (int x = 0; x < VT; ++x) tree_finish4(p, D, b, hk, at_part, r0 + 16 * t + lr, R, node[t], row_ok[t], 16 * x + 4 * lq, tiles.m[t], L, tiles.acc[t][x]);
   }
 }
 
@@ -777,7 +782,7 @@ __global__ __launch_bounds__(256) void tree_rows_kernel(TreeP p) {
       L = fmaf(l_s[w][lr], a, L);
       o += o_s[w][x][lane] * a;
     }
-    tree_finish4(p, D, b, hk, at_part, row, R, node, 16 * x + 4 * lq, M, L, o);
+    tree_finish4(p, D, b, hk, at_part, row, R, node, row_ok, 16 * x + 4 * lq, M, L, o);
   }
 }
 
@@ -816,5 +821,6 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeP p) {
   const int used = min(NG, n);
   for (int x = 1; x < used; ++x) { o += o_s[tid + x * Q]; L += l_s[tid + x * Q]; }
   const int node = r / p.G;
-  tree_store4(p, b, node, hk * p.G + r - node * p.G, 4 * c, L > 0.f ? o / L : (L != L ? f32x4{L, L, L, L} : f32x4{0.f, 0.f, 0.f, 0.f}));
+  const float none = L != L || (L == 0.f && ls[0] != 0.f) ? NAN : 0.f;           // (as tree_quotient; without weights in all parts, and there: 1 in each)
+  tree_store4(p, b, node, hk * p.G + r - node * p.G, 4 * c, L > 0.f ? o / L : f32x4{none, none, none, none});
 }

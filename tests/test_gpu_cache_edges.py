@@ -106,3 +106,35 @@ def test_chosen_blocks_of_other_scales(dtype, d, kv, g, t, n, cap):
         got, chosen = bpd.bpd_sparse_attention(cache, q.cuda(), ints([n]), binding.new_summaries(cache, 32), scale=scale, parent=torch.from_numpy(parent).cuda(), **what)
         assert torch.equal(chosen.cpu(), picks), scale
         ref.check(got, want, off, what=str(scale))
+
+
+# ------------------------------------------------------------------------------------------------ scores that are not finite
+
+# heads of K, heads per head of K, nodes, length, capacity: one part and several of the keys, rows that share keys through LDS and not
+PLACES = [(2, 2, 5, 40, 64), (1, 1, 1, 0, 32), (1, 1, 3, 3000, 8192), (1, 8, 12, 900, 992), (1, 4, 30, 5000, 5056)]
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16), (F32, 64), (BF, 16)], ids=lambda x: str(x).replace("torch.", ""))
+@pytest.mark.parametrize("kv,g,t,n,cap", PLACES)
+@pytest.mark.parametrize("sparse", [False, True], ids=["all", "blocks"])
+def test_all_scores_minus_infinite(dtype, d, kv, g, t, n, cap, sparse):
+    """A node all of whose scores are -inf has no weights (0 / 0): no number, as the formula gives; an absent one stays zero; one that sees a finite score is as ever."""
+    rng = np.random.default_rng(t + n)
+    k, v = rows(rng, 1, cap, kv, d, dtype=dtype), rows(rng, 1, cap, kv, d, dtype=dtype)
+    k[..., 0] = -INF
+    q = rows(rng, 1, t, kv * g, d, dtype=dtype)
+    q[..., 0] = 1.0
+    parent = np.full((1, t), -1, np.int32)
+    if t > 2:
+        parent[0, 1] = -7                          # absent
+        k[0, n + 2, :, 0] = 0.5                    # a finite score of its own
+    what = dict(block=32, first=1, recent=1, top=1) if sparse else None
+    want, off, _ = ref.attention(q, k, v, [n], parent, blocks=what)
+    assert bool(torch.isnan(want[0, 0]).all()) and (t <= 2 or (not bool(want[0, 1].any()) and bool(torch.isfinite(want[0, 2]).all())))
+    off = torch.where(torch.isfinite(off), off, torch.full_like(off, 2.0 ** -20 * float(v.float().abs().max())))   # (the bound is of infinite scores: one key has all the weight, or none does)
+    cache = packed(k, v)
+    if sparse:
+        got, _ = bpd.bpd_sparse_attention(cache, q.cuda(), ints([n]), binding.new_summaries(cache, 32), parent=torch.from_numpy(parent).cuda(), **what)
+    else:
+        got = bpd.bpd_tree_attention(cache, q.cuda(), ints([n]), torch.from_numpy(parent).cuda())
+    ref.check(got, want, off)
