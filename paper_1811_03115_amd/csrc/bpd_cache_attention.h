@@ -35,6 +35,14 @@ struct TreeP {
 
 typedef unsigned long long mask64;
 
+// Where the element (key, dimension c) lies in a sequence's and head's part of a cache in operand order (c % 8 == 0: eight dimensions of K side by side)
+template <int D> __device__ __forceinline__ size_t k_at(int key, int c) {
+  return (size_t)(key >> 5) * (TREE_GROUP * D) + ((key >> 2) & 1) * (16 * D) + (c >> 5) * 512 + (((c >> 3) & 3) * 16 + ((key >> 3) & 3) * 4 + (key & 3)) * 8 + (c & 7);
+}
+template <int D> __device__ __forceinline__ size_t v_at(int key, int c) {
+  return (size_t)(key >> 5) * (TREE_GROUP * D) + (c >> 4) * 512 + (((key >> 3) & 3) * 16 + (c & 15)) * 8 + (key & 7);
+}
+
 // Ancestors of node `lane` (bits), and whether it is there, by all 64 lanes of a wave: after round n a node knows 2^n of its ancestors.
 __device__ __forceinline__ void tree_ancestors(const TreeP& tp, int b, int there, int lane, mask64& anc, bool& ok) {
   if (!tp.parent && !tp.tree) {                  // a chain
@@ -224,9 +232,10 @@ struct TreeTiles {
   }
   // kf, vf: the item's operands; at: this lane's first key among the drafts; edge: whether any key of the item is a draft (the same for the whole wave); vis: whether
   // row t sees the item's committed keys; seen: the drafts that it sees; q(t, x): its operand
-  // SAFE: values one by one (value(key, dimension)), for the keys that a row sees and no others: a product's zero times what is not finite is not zero
-  template <bool SAFE, typename Q, typename QL, typename V>
-  __device__ __forceinline__ void item(const u32x4 (&kf)[2 * KS], const u32x4 (&vf)[VT], int at, bool edge, const bool (&vis)[MT], const mask64 (&seen)[MT], float scale, const Q& q, const QL& ql, const V& value) {
+  // SAFE: values one by one (value(key, dimension)), for the keys that a row sees and no others: a product's zero times what is not finite is not zero.  Nor are zeros that a pair of an
+  // fp32 query adds: scores that are no number come once more, of the query as it is (score(t, key of this lane)).
+  template <bool SAFE, typename Q, typename QL, typename V, typename S>
+  __device__ __forceinline__ void item(const u32x4 (&kf)[2 * KS], const u32x4 (&vf)[VT], int at, bool edge, const bool (&vis)[MT], const mask64 (&seen)[MT], float scale, const Q& q, const QL& ql, const V& value, const S& score) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       f32x4 s[2];
@@ -240,6 +249,12 @@ struct TreeTiles {
           if constexpr (QF32) a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, ql(t, x), a, 0, 0, 0);
         }
         s[u] = a;
+      }
+      if constexpr (SAFE && QF32) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) if (s[u][r] != s[u][r]) s[u][r] = score(t, 4 * u + r);
       }
       if (edge) {
 #pragma unroll
@@ -325,10 +340,6 @@ __device__ __forceinline__ void tree_blank(u32x4 (&vf)[VT], int at, mask64 prese
     for (int x = 0; x < VT; ++x) vf[x][w] &= known;
   }
 }
-// Where dimension c of a key's values lies in a sequence's and head's part of a cache in operand order
-template <int D> __device__ __forceinline__ size_t tree_v_at(int key, int c) {
-  return (size_t)(key >> 5) * (TREE_GROUP * D) + (c >> 4) * 512 + (((key >> 3) & 3) * 16 + (c & 15)) * 8 + (key & 7);
-}
 // Row r of a (sequence, key head) pair: its node, what it sees of the drafts, whether it is there
 __device__ __forceinline__ void tree_row(const TreeP& p, int r, int R, mask64 anc, int& node, mask64& seen, bool& ok) {
   node = r < R ? r / p.G : 0;
@@ -343,6 +354,14 @@ __device__ __forceinline__ void tree_q_operand(const TreeP& p, int b, int hk, in
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] *= p.sign;    // (of the scale: the maximum is that of the products)
   tree_pair(v, hi, lo);
+}
+// q . K_key of a row that is there, term by term; K: the sequence's and head's keys in operand order
+template <int D>
+__device__ __forceinline__ float tree_score(const TreeP& p, int b, int hk, int r, int node, const bf16_t* K, int key) {
+  float sum = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < D; ++c) sum = fmaf(p.sign * tree_q1(p, b, node, hk * p.G + r - node * p.G, c), bf2f(K[k_at<D>(key, c)]), sum);
+  return sum;
 }
 // What a row's sums make of it.  No weights at all: an absent node's zeros, or (there: all of its scores are -inf) no number, 0 / 0
 __device__ __forceinline__ f32x4 tree_quotient(const f32x4& o, float L, bool there) {
@@ -441,7 +460,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_kernel(TreeP p) {
     const bool edge = 32 * g + 32 > len;
     if (!SAFE && edge) tree_blank<VT>(vf, at, present);
     tiles.template item<SAFE>(k, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; },
-                              [&](int t, int x) { return ql[QF32 ? t : 0][x]; }, [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + tree_v_at<D>(32 * g + j, c)]); });
+                              [&](int t, int x) { return ql[QF32 ? t : 0][x]; }, [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + v_at<D>(32 * g + j, c)]); },
+                              [&](int t, int j) { return row_ok[t] ? tree_score<D>(p, b, hk, 16 * t + lr, node[t], (const bf16_t*)p.K + own, 32 * g + 8 * lq + j) : 0.f; });
   };
   {
     int i = i0 + wave, g = i < i1 ? __builtin_amdgcn_readfirstlane(it.group(i)) : 0;
@@ -611,7 +631,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_attention_rows_kernel(TreeP p
       const bool edge = 32 * g + 32 > len;
       if (!SAFE && edge) tree_blank<VT>(vf, at, present);
       tiles.template item<SAFE>(kf, vf, at, edge, vis, seen, p.scale, [&](int t, int x) { return qh[t][x]; }, [&](int t, int x) { return ql[QF32 ? t : 0][x]; },
-                                [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + tree_v_at<D>(32 * g + j, c)]); });
+                                [&](int j, int c) { return bf2f(((const bf16_t*)p.V)[own + v_at<D>(32 * g + j, c)]); },
+                                [&](int t, int j) { return row_ok[t] ? tree_score<D>(p, b, hk, r0 + 16 * t + lr, node[t], (const bf16_t*)p.K + own, 32 * g + 8 * lq + j) : 0.f; });
       if (i + 1 < i1) put(buf ^ 1);
       __syncthreads();
       g = gn;

@@ -3,14 +3,6 @@
 #pragma once
 #include "bpd_cache_attention.h"
 
-// Where the element (key, dimension c) lies in a sequence's and head's part of a cache in operand order (c % 8 == 0: eight dimensions of K side by side)
-template <int D> __device__ __forceinline__ size_t k_at(int key, int c) {
-  return (size_t)(key >> 5) * (TREE_GROUP * D) + ((key >> 2) & 1) * (16 * D) + (c >> 5) * 512 + (((c >> 3) & 3) * 16 + ((key >> 3) & 3) * 4 + (key & 3)) * 8 + (c & 7);
-}
-template <int D> __device__ __forceinline__ size_t v_at(int key, int c) {
-  return (size_t)(key >> 5) * (TREE_GROUP * D) + (c >> 4) * 512 + (((key >> 3) & 3) * 16 + (c & 15)) * 8 + (key & 7);
-}
-
 // ------------------------------------------------------------------------------------------------ rows into a cache
 
 struct RowsP { const void* data; int f32, vec; long layer, seq, row, head; };      // vec: eight elements can be loaded at once

@@ -138,3 +138,30 @@ def test_all_scores_minus_infinite(dtype, d, kv, g, t, n, cap, sparse):
     else:
         got = bpd.bpd_tree_attention(cache, q.cuda(), ints([n]), torch.from_numpy(parent).cuda())
     ref.check(got, want, off)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv,g,t,n,cap", PLACES[:1] + PLACES[2:])
+def test_infinite_keys_under_fp32_queries(d, kv, g, t, n, cap):
+    """Keys with an infinite dimension under queries of fp32: a score of -inf has no weight and leaves the others theirs, one of +inf leaves no number, whatever the queries round to."""
+    rng = np.random.default_rng(t + n + d)
+    k, v = rows(rng, 1, cap, kv, d), rows(rng, 1, cap, kv, d)
+    q = rows(rng, 1, t, kv * g, d, dtype=F32)
+    q[..., 0] = 1.0                                # exact in fewer bits
+    q[..., 1] = 1.0 + 2.0 ** -20
+    bad = [i for i in range(0, n, 7)]
+    k[0, bad, :, 0] = -INF
+    k[0, [i + 1 for i in bad if i + 1 < n], :, 1] = -INF
+    want = ref.attention(q, k, v, [n], None)[0]
+    fine = [i for i in range(n + t) if bool(torch.isfinite(k[0, i]).all())]
+    seen = len([i for i in fine if i < n])
+    kept = torch.tensor(fine)
+    less, off, _ = ref.attention(q, k[:, kept], v[:, kept], [seen], None)
+    assert torch.allclose(want, less, rtol=1e-12, atol=1e-14)
+    off = off * ((n + t) / (seen + 1))             # (as many terms as there are keys)
+    out = torch.empty(q.shape, dtype=F32, device="cuda")
+    bpd.bpd_tree_attention(packed(k, v), q.cuda(), ints([n]), out=out)
+    ref.check(out, less, off)
+    k[0, n, 0, 0] = INF                            # the first node's own key: for it and all below it
+    got = bpd.bpd_tree_attention(packed(k, v), q.cuda(), ints([n]), out=out).cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(ref.attention(q, k, v, [n], None)[0]))
