@@ -137,9 +137,7 @@ BoundP bound_args(TreeP& p, const bpd_cache& c, const bpd_blocks& blocks, unsign
 // What bpd_tree_attention and bpd_sparse_attention check alike; null: nothing is wrong
 const char* attention_wrong(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, int B, int T, int heads, float scale) {
   if (const char* w = cache_wrong(c)) return w;
-  if (B < 0 || B > c->max_batch) return "attention: B outside 0..max_batch";
-  if (T < 0 || T > BPD_TREE_MAX) return "attention: T outside 0..BPD_TREE_MAX";
-  if (heads < 1 || heads % c->n_kv_heads || heads / c->n_kv_heads > 64) return "attention: heads are 1 to 64 times the cache's";
+  if (const char* w = attention_sizes_wrong(*c, B, T, heads)) return w;
   if (!(scale == scale) || std::isinf(scale)) return "attention: scale is not finite";
   if (B == 0 || T == 0) return nullptr;          // (nothing is read)
   if (const char* w = rows_wrong(q)) return w;
@@ -204,13 +202,13 @@ size_t bpd_cache_bytes(const bpd_cache* c) {
 }
 
 size_t bpd_summaries_bytes(const bpd_cache* c, int block) {
-  if (cache_sizes_wrong(c) || block_wrong(*c, block)) return 0;
+  if (cache_sizes_wrong(c) || block_wrong(*c, block) || c->capacity / block > BPD_BLOCKS_MAX) return 0;
   return summaries_elements(*c, block) * cache_element(*c);
 }
 
 size_t bpd_attention_workspace_bytes(const bpd_cache* c, int B, int T, int heads, int block) {
-  if (cache_sizes_wrong(c) || B < 1 || T < 1 || T > BPD_TREE_MAX || heads < 1 || heads % c->n_kv_heads) return 0;
-  if (block && block_wrong(*c, block)) return 0;
+  if (cache_sizes_wrong(c) || B < 1 || attention_sizes_wrong(*c, B, T, heads) || T < 1) return 0;
+  if (block && (block_wrong(*c, block) || c->capacity / block > BPD_BLOCKS_MAX)) return 0;
   return plan_attention(*c, B, T, heads, block, compute_units()).bytes;
 }
 

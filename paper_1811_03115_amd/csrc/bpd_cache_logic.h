@@ -28,6 +28,12 @@ inline const char* cache_wrong(const bpd_cache* c) {
   if (!c->k || !c->v || ((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15)) return "cache: k or v null, or not aligned to 16 bytes";
   return nullptr;
 }
+inline const char* attention_sizes_wrong(const bpd_cache& c, int B, int T, int heads) {
+  if (B < 0 || B > c.max_batch) return "attention: B outside 0..max_batch";
+  if (T < 0 || T > BPD_TREE_MAX) return "attention: T outside 0..BPD_TREE_MAX";
+  if (heads < 1 || heads % c.n_kv_heads || heads / c.n_kv_heads > 64) return "attention: heads are 1 to 64 times the cache's";
+  return nullptr;
+}
 inline const char* block_wrong(const bpd_cache&, int block) {
   return block == 32 || block == 64 || block == 128 ? nullptr : "blocks: 32, 64 or 128 rows";
 }
