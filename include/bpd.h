@@ -392,7 +392,7 @@ int bpd_cache_store(const bpd_cache* cache, const bpd_rows* k, const bpd_rows* v
  *   q, out  rows of n_heads heads (a multiple of the cache's: heads in a row share a key head)
  *   out[b][i][h] = sum_j p_j V_j,  p = softmax of scale * q . K_j over the prefix and node i's ancestors and itself;
  *       0 for absent nodes (NaN, 0 / 0, for one all of whose scores are -inf).  Sums, maxima and weights in fp32.  What a node does not see does not matter to it, finite or not.
- * Chains of one node are plain decoding.  T <= BPD_TREE_MAX; n_heads / n_kv_heads <= 64; B or T of 0 does nothing.
+ * Chains of one node are plain decoding.  T <= BPD_TREE_MAX; n_heads / n_kv_heads <= 64; scale and scale * log2(e) finite; B or T of 0 does nothing.
  * Errors: BPD_E_ARG, BPD_E_CAPACITY (workspace), BPD_E_HIP. */
 int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows* out, const int32_t* length,
                        const int32_t* parent, int B, int T, int n_heads, float scale,

@@ -134,11 +134,12 @@ BoundP bound_args(TreeP& p, const bpd_cache& c, const bpd_blocks& blocks, unsign
   return bp;
 }
 
+constexpr float LOG2_E = 1.44269504088896340736f;
 // What bpd_tree_attention and bpd_sparse_attention check alike; null: nothing is wrong
 const char* attention_wrong(const bpd_cache* c, const bpd_rows* q, const bpd_rows* out, const int32_t* length, int B, int T, int heads, float scale) {
   if (const char* w = cache_wrong(c)) return w;
   if (const char* w = attention_sizes_wrong(*c, B, T, heads)) return w;
-  if (!(scale == scale) || std::isinf(scale)) return "attention: scale is not finite";
+  if (!std::isfinite(scale * LOG2_E)) return "attention: scale is not finite, or not times log2(e)";
   if (B == 0 || T == 0) return nullptr;          // (nothing is read)
   if (const char* w = rows_wrong(q)) return w;
   if (const char* w = rows_wrong(out)) return w;
@@ -151,7 +152,7 @@ TreeP attention_args(const bpd_cache& c, const bpd_rows& q, const bpd_rows& out,
   p.K = c.k; p.V = c.v;
   p.B = B; p.T = T; p.H = heads; p.kv = c.n_kv_heads; p.G = heads / c.n_kv_heads; p.cap = c.capacity;
   p.length = length; p.parent = parent;
-  p.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.44269504088896340736f;
+  p.scale = scale == 0.f ? 1.f : fabsf(scale) * LOG2_E;
   p.sign = scale > 0.f ? 1.f : (scale < 0.f ? -1.f : 0.f);
   p.q_f32 = q.dtype == BPD_F32; p.o_f32 = out.dtype == BPD_F32;
   p.vec = rows_aligned(q) && rows_aligned(out);
