@@ -433,7 +433,7 @@ int bpd_sparse_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_ro
  *   new_length [B]         length + accepted (a negative length: nothing is accepted, and it stays)
  *   cache                  NULL, or the cache whose rows length + path[m] move to length + m, in all layers; nodes whose rows
  *                          are past its capacity are then absent
- * The four results must not overlap what is read.  Errors: BPD_E_ARG, BPD_E_CAPACITY (n_layers over 65535), BPD_E_HIP. */
+ * The four results must not overlap what is read, nor each other.  Errors: BPD_E_ARG, BPD_E_CAPACITY (n_layers over 65535), BPD_E_HIP. */
 int bpd_tree_accept(const int32_t* parent, const int32_t* token, const int32_t* expect, const int32_t* best,
                     const int32_t* length, const int32_t* room, int eos_id, int B, int T, int32_t* path,
                     int32_t* accepted, int32_t* next, int32_t* new_length, const bpd_cache* cache, void* hip_stream);

@@ -285,11 +285,14 @@ int bpd_tree_accept(const int32_t* parent, const int32_t* token, const int32_t* 
   if (B == 0) return BPD_OK;
   if (!expect || !length || !accepted || !next || !new_length || (T > 0 && (!parent || !token || !best || !path))) return refuse(BPD_E_ARG, "bpd_tree_accept: null argument");
   // (every workgroup reads the inputs, one writes the results)
-  const struct { const void* p; size_t n; } in[] = {{parent, (size_t)B * T}, {token, (size_t)B * T}, {best, (size_t)B * T}, {expect, (size_t)B}, {length, (size_t)B}, {room, room ? (size_t)B : 0}};
-  const struct { const void* p; size_t n; } res[] = {{path, (size_t)B * T}, {accepted, (size_t)B}, {next, (size_t)B}, {new_length, (size_t)B}};
-  for (const auto& r : res)
-    for (const auto& i : in)
-      if (i.n && r.n && (const char*)r.p < (const char*)i.p + 4 * i.n && (const char*)i.p < (const char*)r.p + 4 * r.n) return refuse(BPD_E_ARG, "bpd_tree_accept: results overlap what is read");
+  struct Ints { const void* p; size_t n; };
+  const Ints in[] = {{parent, (size_t)B * T}, {token, (size_t)B * T}, {best, (size_t)B * T}, {expect, (size_t)B}, {length, (size_t)B}, {room, room ? (size_t)B : 0}};
+  const Ints res[] = {{path, (size_t)B * T}, {accepted, (size_t)B}, {next, (size_t)B}, {new_length, (size_t)B}};
+  auto meet = [](const Ints& a, const Ints& b) { return a.n && b.n && (const char*)a.p < (const char*)b.p + 4 * b.n && (const char*)b.p < (const char*)a.p + 4 * a.n; };
+  for (const Ints& r : res) {
+    for (const Ints& i : in) if (meet(r, i)) return refuse(BPD_E_ARG, "bpd_tree_accept: results overlap what is read");
+    for (const Ints* o = res; o < &r; ++o) if (meet(r, *o)) return refuse(BPD_E_ARG, "bpd_tree_accept: results overlap each other");
+  }
   AcceptP p{parent, token, expect, best, length, room, path, accepted, next, new_length, eos_id, T, B, nullptr, nullptr, 0, 1, 0};
   const hipStream_t s = (hipStream_t)hip_stream;
   dim3 grid(1, 1, B);
