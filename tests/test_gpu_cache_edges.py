@@ -165,3 +165,62 @@ def test_infinite_keys_under_fp32_queries(d, kv, g, t, n, cap):
     k[0, n, 0, 0] = INF                            # the first node's own key: for it and all below it
     got = bpd.bpd_tree_attention(packed(k, v), q.cuda(), ints([n]), out=out).cpu()
     assert torch.equal(torch.isnan(got), torch.isnan(ref.attention(q, k, v, [n], None)[0]))
+
+
+# ------------------------------------------------------------------------------------------------ captured steps that carry their state
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 16)], ids=lambda x: str(x).replace("torch.", ""))
+def test_replays_summarise_what_the_one_before_has_added(dtype, d):
+    """A serving step in a graph: rows stored, chosen blocks with the rows that the replay before has accepted as `added`, the tree verified, lengths moved on.  Each replay against the
+    same step called directly on a state of its own, and summaries against those of the keys."""
+    rng = np.random.default_rng(14)
+    b, kv, g, t, cap, block = 3, 2, 2, 6, 320, 32
+    names = ("nk", "nv", "q", "parent", "token", "best", "expect")
+
+    def state(k, v):
+        s = dict(cache=tuple(x.clone() for x in packed(k, v)), length=ints([40, 0, 95]), added=ints([1 << 30] * b))
+        s.update(nk=torch.zeros((b, t, kv, d), dtype=dtype, device="cuda"), nv=torch.zeros((b, t, kv, d), dtype=dtype, device="cuda"), q=torch.zeros((b, t, kv * g, d), dtype=dtype, device="cuda"))
+        s.update({n: torch.zeros((b, t), dtype=torch.int32, device="cuda") for n in ("parent", "token", "best")}, expect=ints([0] * b))
+        s["summaries"] = binding.new_summaries(s["cache"], block)
+        return s
+
+    def step(s):
+        bpd.bpd_cache_store(s["cache"], s["nk"], s["nv"], s["length"])
+        out, chosen = bpd.bpd_sparse_attention(s["cache"], s["q"], s["length"], s["summaries"], block=block, first=0, recent=1, top=2, parent=s["parent"], added=s["added"])
+        path, accepted, following, after = bpd.bpd_tree_accept(s["parent"], s["token"], s["expect"], s["best"], s["length"], cache=s["cache"])
+        s["length"].copy_(after)
+        s["added"].copy_(accepted)
+        return out, chosen, path, accepted
+
+    k, v = rows(rng, b, cap, kv, d, dtype=dtype), rows(rng, b, cap, kv, d, dtype=dtype)
+    warm, one, two = state(k, v), state(k, v), state(k, v)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(warm)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = step(one)
+    for turn in range(60):
+        parent = np.array([[-1] + [int(rng.integers(max(0, i - 2), i)) for i in range(1, t)] for _ in range(b)], np.int32)
+        new = dict(nk=rows(rng, b, t, kv, d, dtype=dtype), nv=rows(rng, b, t, kv, d, dtype=dtype), q=rows(rng, b, t, kv * g, d, dtype=dtype), parent=torch.from_numpy(parent))
+        new.update({n: torch.from_numpy(rng.integers(0, 2, tuple(one[n].shape)).astype(np.int32)) for n in ("token", "best", "expect")})
+        for s in (one, two):
+            for n in names:
+                s[n].copy_(new[n])
+        before = two["length"].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(res, step(two)):
+            assert torch.equal(x, y), turn
+        for n in ("length", "added"):
+            assert torch.equal(one[n], two[n])
+        keys = ref.unpack(*(x.cpu() for x in two["cache"]))[0]
+        for s in (one, two):
+            kept = ref.summaries_unpacked(s["summaries"].cpu(), cap // block)
+            for i, n in enumerate(before.tolist()):
+                assert torch.equal(kept[i, :, :n // block], ref.summaries(keys[i:i + 1], block)[0, :, :n // block]), (turn, i)
+        if max(two["length"].tolist()) > cap - t:
+            break
+    assert all(n // block > m // block for n, m in zip(two["length"].tolist(), (40, 0, 95)))       # (blocks have become complete)
