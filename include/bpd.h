@@ -254,7 +254,9 @@ int bpd_set_local_attention(bpd_ctx* ctx, int query_block, int memory_len);
  * `first` and the last `recent` complete blocks of `block` rows (32, 64 or 128), the `top` others with the largest bound of its
  * scores per head, and what is behind the last complete block; and the step's own rows as ever.  For very long outputs: eight images with
  * 29 blocks of 32 are faster from some 16000 positions on (23000: 472 us a step with all keys, 396), below that the kernel of all
- * layers that full attention has outweighs the keys left out (2900: 194 us, 314).  block = 0 (the rest is ignored) restores attention to all keys, the default; the setting may change
+ * layers that full attention has outweighs the keys left out (2900: 194 us, 314).  Once a context has captured a call, replays may have committed what its direct steps
+ * do not know of: they make all summaries anew, in every layer (room for 24000 positions, a step at 2900 382 us and then 1060, at 23000 390 and 1361); captured
+ * steps do not.  block = 0 (the rest is ignored) restores attention to all keys, the default; the setting may change
  * between steps, and applies to later bpd_step / bpd_step_tree / bpd_decode / bpd_debug_step_logits calls (whose layers then run kernel by
  * kernel).
  *   buffer [device] caller-owned, 256-byte aligned, bpd_sparse_buffer_bytes(ctx, block), not shared with another context; it must stay
@@ -391,7 +393,10 @@ int bpd_cache_store(const bpd_cache* cache, const bpd_rows* k, const bpd_rows* v
  *       capacity, all nodes of a sequence with length[b] < 0.
  *   q, out  rows of n_heads heads (a multiple of the cache's: heads in a row share a key head)
  *   out[b][i][h] = sum_j p_j V_j,  p = softmax of scale * q . K_j over the prefix and node i's ancestors and itself;
- *       0 for absent nodes (NaN, 0 / 0, for one all of whose scores are -inf).  Sums, maxima and weights in fp32.  What a node does not see does not matter to it, finite or not.
+ *       0 for absent nodes (NaN, 0 / 0, for one all of whose scores are -inf).  Scores, maxima and sums in fp32.  Over caches in operand order the weights, and queries of fp32, enter
+ *       their products as pairs of bf16 numbers, which keep them to 2^-17: results of fp32 are off by some 2e-6 of the values' size (fp32 throughout:
+ *       3e-7 to 8e-7), of those of bf16 one in 500 is the second nearest number; all other caches: fp32 throughout.  Weights are up to 2^8 before they are divided by
+ *       their sum: values whose sum over the keys passes 2^119 may come out infinite.  What a node does not see does not matter to it, finite or not.
  * Chains of one node are plain decoding.  T <= BPD_TREE_MAX; n_heads / n_kv_heads <= 64; scale and scale * log2(e) finite; B or T of 0 does nothing.
  * Errors: BPD_E_ARG, BPD_E_CAPACITY (workspace), BPD_E_HIP. */
 int bpd_tree_attention(const bpd_cache* cache, const bpd_rows* q, const bpd_rows* out, const int32_t* length,

@@ -175,7 +175,7 @@ def new_cache(max_batch: int, n_kv_heads: int, head_dim: int, capacity: int, dty
 
 
 def new_summaries(cache, block: int):
-    """Summaries of one layer's blocks for bpd_sparse_attention, zeros."""
+    """Room for the summaries of one layer's blocks, zeros: the first bpd_sparse_attention that gets them has added=None, which makes all of them."""
     import torch
     (_, _, _, _, b, h, d, cap), k, _ = _cache(cache, 0)
     if block not in (32, 64, 128):
@@ -543,7 +543,8 @@ class Context:
     @staticmethod
     def bpd_sparse_attention(cache, q, length, summaries, block: int, first: int, recent: int, top: int, parent=None, added=None, layer: int = 0,
                              scale: Optional[float] = None, out=None, chosen=None, workspace=None):
-        """As bpd_tree_attention, over chosen blocks; summaries: binding.new_summaries(), one per layer.  Returns (out, chosen [B, kv heads, T, words] int32)."""
+        """As bpd_tree_attention, over chosen blocks; summaries: binding.new_summaries(), one per layer; added [B]: rows committed since the call before with them, None: all
+        (the first call).  Returns (out, chosen [B, kv heads, T, words] int32)."""
         if block not in (32, 64, 128):
             raise _bad("block: 32, 64 or 128 rows")
         device, c, args, keep, ws, n, out = _attention(cache, layer, q, length, parent, scale, out, workspace, block)

@@ -215,7 +215,8 @@ __device__ __forceinline__ int tree_list(const unsigned* chosen, int words, int 
 //                          it): maxima over the four lanes of a row, and multiplications of all results, are then rare.  Sums stay in their lanes until the end.
 //   out^T += V^T P^T       the probabilities as they lie are the second operand
 // Queries of bf16 are exact, those of fp32 a pair.  Probabilities go in as a pair hi + lo: as single bf16 numbers their rounding adds as much error as that of the bf16
-// results (sum over keys of p (1 +- 2^-9) v), which the pair's second product takes to 2^-17.
+// results (sum over keys of p (1 +- 2^-9) v), which the pair's second product takes to 2^-17.  (Against 64 bits, 40 and 2999 keys: fp32 results 2.1e-6 and 2.3e-6 of their size, fp32 weights
+// 0.3e-6 and 0.8e-6; bf16 results 0.0017 either way, 0.2% of them the second nearest number instead of 0 to 0.09%.)
 constexpr float TREE_SLACK = 8.f;
 template <int D, int MT, bool QF32>
 struct TreeTiles {
